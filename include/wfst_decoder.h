@@ -10,7 +10,8 @@
  * Conventions
  *   - Every call returns a status (0 = WFST_OK, negative = error).  Nothing throws or aborts
  *     across this boundary.  wfst_last_error() gives a library-owned message for the last
- *     failing call on that decoder (or on creation when passed NULL).
+ *     failing call on that decoder (when passed NULL: for the calling thread's last failing creation
+ *     or call that takes no decoder).
  *   - "host" / "device" on a pointer says where the memory lives.  The library never takes
  *     ownership of caller memory; graph arrays are copied during create.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Work is
@@ -384,6 +385,136 @@ int32_t wfst_get_lattice_noalloc(wfst_decoder *dec, int32_t ch, const void *logl
                                  int32_t *tok_state, float *tok_cost, int64_t tok_cap, int64_t *frame_off,
                                  wfst_lattice_link *links, int64_t link_cap,
                                  int64_t *n_tokens, int64_t *n_links, void *stream);
+
+/*
+ * Beside the decoder: the output layer that makes the log-likelihoods out of an encoder's hidden states,
+ * and the probabilities of what was decoded.  (The paper's pipeline is feature extractor -> acoustic model ->
+ * decoder; it describes neither of these two, the definitions are this library's own.)
+ *
+ * These calls need no decoder and keep nothing between calls.  All pointers in the argument structs are DEVICE
+ * memory of the GPU that `stream` belongs to, which must be the calling thread's current device; the structs
+ * themselves are read during the call.  Work is enqueued on `stream`; no call synchronises, allocates or copies to
+ * the host, and every one may be recorded into a graph.  Calls from several threads and on several streams may
+ * overlap, as long as none writes what another reads or writes.  Results do not depend on the launch: the same
+ * call gives the same bits.  On an error nothing is enqueued, and wfst_last_error(NULL) says why (on the
+ * thread that made the call).  Element types are WFST_LOGLIKE_F32 / _F16 / _BF16; sums, maxima and
+ * softmax statistics are held in fp32, and a 16-bit result is rounded once, at the end.  Strides count elements.
+ * Errors: INVALID_ARG, HIP.
+ */
+enum { WFST_ACT_NONE = 0, WFST_ACT_RELU = 1, WFST_ACT_SILU = 2, WFST_ACT_GELU = 3 };
+
+/*
+ * y[m][n] = residual[m][n] + scale * act(sum_k x[m][k] * w[n][k] + bias[n])
+ * with act one of WFST_ACT_*: none; relu max(z, 0); silu z / (1 + e^-z); gelu z/2 (1 + erf(z / sqrt 2)).
+ *   rows >= 0 (0: nothing is done), k >= 1, n >= 1.  Row m of x starts at element m * x_stride (x_stride >= 0: a
+ *   row may be shared or overlap the next), likewise w; y_stride and residual_stride >= n.
+ *   bias and residual may be NULL.  dtype: of x and w; bias_dtype: of bias; out_dtype: of y and residual.
+ *   y must not overlap what is read, except that it may be the residual itself (same address and stride).
+ */
+typedef struct {
+  const void *x;                  /* [rows][k] */
+  const void *w;                  /* [n][k] */
+  const void *bias;               /* [n] or NULL */
+  const void *residual;           /* [rows][n] or NULL */
+  void *y;                        /* [rows][n] */
+  int64_t rows;
+  int64_t x_stride, w_stride, residual_stride, y_stride;
+  int32_t k, n;
+  int32_t dtype, bias_dtype, out_dtype;
+  int32_t activation;
+  float scale;
+} wfst_linear_args;
+
+int32_t wfst_linear(const wfst_linear_args *args, void *stream);
+
+/*
+ * The output layer: z = x w^T + bias, out[s][t][c] = z[c] - log(sum_c' e^z[c']) - log_prior[c], the `loglikes` argument
+ * of wfst_decode_batch ([seqs] = B, [frames] = T, [v] = V) and wfst_advance_chunk.
+ *   Frame t of sequence s is the k elements from s * x_seq_stride + t * x_stride (>= 0 both), so a time-major
+ *   [T][B][k] tensor is taken as it is; likewise its v results (out_stride >= v; the rows must not overlap).
+ *   lengths (int32 [seqs], or NULL = all frames): frames t >= lengths[s] are neither read nor written.
+ *   log_prior (float [v], or NULL): log probabilities of the classes, taken off so that a hybrid decoder gets
+ *   likelihoods up to a constant.  1 <= v <= 2048 (the decoder's own limit), k >= 1.
+ *   A frame with a NaN or +inf in z, or -inf in all of it, gives NaN for the whole row; a -inf in z gives -inf.
+ */
+typedef struct {
+  const void *x;                  /* [seqs][frames][k] */
+  const void *w;                  /* [v][k] */
+  const void *bias;               /* [v] or NULL */
+  const float *log_prior;         /* [v] or NULL */
+  const int32_t *lengths;         /* [seqs] or NULL */
+  void *out;                      /* [seqs][frames][v] */
+  int64_t x_seq_stride, x_stride, w_stride, out_seq_stride, out_stride;
+  int32_t seqs, frames, k, v;
+  int32_t dtype, bias_dtype, out_dtype;
+} wfst_loglikes_args;
+
+int32_t wfst_loglikes(const wfst_loglikes_args *args, void *stream);
+
+/*
+ * Of each row of scores x[0..v) (logits, or log-likelihoods): lse = log(sum_j e^x[j]), log-probabilities x[j] - lse
+ * of `given` tokens and of the `top` best ones, and the entropy -sum_j p[j] log p[j] with p[j] = e^(x[j] - lse).
+ *   Row (s, t) of the scores starts at element s * seq_stride + t * stride (>= 0 both); tokens and all outputs are
+ *   contiguous over rows (s, t).  lengths as in wfst_loglikes: rows t >= lengths[s] are neither read nor written.
+ *   tokens: int32, -1 = none (log-probability 0); any other value outside [0, v) gives NaN.
+ *   top_ids: by falling score, equal scores by the lower index; a NaN counts as larger than every number.
+ *   stats: the row's maximum and the log of sum_j e^(x[j] - maximum), whose sum lse is, for the backward call: with
+ *   scores far from 0 the sum of the two no longer holds what each of them does.
+ *   Any output may be NULL (logprobs too if given == 0, the top ones if top == 0).
+ *   1 <= v <= 2^30, 0 <= given <= 4096, 0 <= top <= min(v, 64).
+ *   A row with a NaN or +inf gives NaN for lse, entropy and log-probabilities.  A row of -inf only (everything
+ *   ruled out) gives lse -inf, entropy 0, log-probabilities -inf and a maximum of -inf.
+ *   workspace: wfst_token_logprobs_workspace(rows, v, top) bytes (rows = seqs * frames), 16-byte aligned, used by this call alone
+ *   until the stream has finished it; may be NULL if that is 0.
+ */
+typedef struct {
+  const void *scores;             /* [seqs][frames][v] */
+  const int32_t *tokens;          /* [seqs][frames][given] */
+  const int32_t *lengths;         /* [seqs] or NULL */
+  float *logprobs;                /* [seqs][frames][given] */
+  float *lse;                     /* [seqs][frames] */
+  float *entropy;                 /* [seqs][frames] */
+  float *stats;                   /* [seqs][frames][2] */
+  int32_t *top_ids;               /* [seqs][frames][top] */
+  float *top_logprobs;            /* [seqs][frames][top] */
+  void *workspace;
+  int64_t workspace_bytes;
+  int64_t seq_stride, stride;
+  int32_t seqs, frames, v, given, top;
+  int32_t dtype;
+} wfst_token_logprobs_args;
+
+int64_t wfst_token_logprobs_workspace(int64_t rows, int32_t v, int32_t top);
+int32_t wfst_token_logprobs(const wfst_token_logprobs_args *args, void *stream);
+
+/*
+ * The gradient of wfst_token_logprobs with respect to its scores:
+ *   grad_scores[j] = p[j] * (grad_lse - sum grad_logprobs - sum grad_top - grad_entropy * (log p[j] + entropy))
+ *                    + the grad_logprobs of the tokens that are j + the grad_top of the top ones that are j
+ * (the indices of the top ones are constants).  A token outside [0, v) has no gradient; a token given several times
+ * has the sum of its gradients; a row of -inf only has the gradient 0; a -inf among finite scores takes the formula's value
+ * with p[j] = 0.  stats (always) and entropy (if grad_entropy is given) are the forward call's.  Gradients that are
+ * NULL count as 0.  grad_scores has the scores' type and may be the scores themselves (same address and strides), and must
+ * not overlap anything else.  Frames t >= lengths[s] are neither read nor written.
+ */
+typedef struct {
+  const void *scores;             /* [seqs][frames][v] */
+  const int32_t *tokens;          /* [seqs][frames][given] */
+  const int32_t *lengths;         /* [seqs] or NULL */
+  const float *stats;             /* [seqs][frames][2] */
+  const float *entropy;           /* [seqs][frames]; may be NULL without grad_entropy */
+  const int32_t *top_ids;         /* [seqs][frames][top] */
+  const float *grad_logprobs;     /* [seqs][frames][given] or NULL */
+  const float *grad_lse;          /* [seqs][frames] or NULL */
+  const float *grad_entropy;      /* [seqs][frames] or NULL */
+  const float *grad_top;          /* [seqs][frames][top] or NULL */
+  void *grad_scores;              /* [seqs][frames][v] */
+  int64_t seq_stride, stride, grad_seq_stride, grad_stride;
+  int32_t seqs, frames, v, given, top;
+  int32_t dtype;
+} wfst_token_logprobs_backward_args;
+
+int32_t wfst_token_logprobs_backward(const wfst_token_logprobs_backward_args *args, void *stream);
 
 /*
  * Test and measurement hooks.  All outputs are HOST memory; each call synchronises the

@@ -26,7 +26,8 @@ EXPORTS = ["wfst_decoder_create", "wfst_decoder_destroy", "wfst_decode_batch", "
            "wfst_debug_frame_digests",
            "wfst_debug_get_tokens", "wfst_debug_get_token_pairs", "wfst_get_counters", "wfst_debug_phase_ticks", "wfst_debug_set_phase_timing", "wfst_debug_set_cluster_size", "wfst_debug_set_cluster_waits", "wfst_debug_set_cluster_memory",
            "wfst_debug_last_launch", "wfst_debug_last_kernel", "wfst_set_launch_workgroups", "wfst_device_bytes",
-           "wfst_last_kernel_ms", "wfst_last_error"]
+           "wfst_last_kernel_ms", "wfst_last_error",
+           "wfst_linear", "wfst_loglikes", "wfst_token_logprobs", "wfst_token_logprobs_workspace", "wfst_token_logprobs_backward"]
 
 
 class WfstError(RuntimeError):
@@ -81,6 +82,33 @@ class wfst_lattice_link(C.Structure):
     _fields_ = [("src", C.c_int32), ("dst", C.c_int32), ("ilabel", C.c_int32), ("olabel", C.c_int32),
                 ("graph_cost", C.c_float), ("acoustic_cost", C.c_float), ("cost", C.c_float),
                 ("frame", C.c_int32)]
+
+
+class wfst_linear_args(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("x", "w", "bias", "residual", "y")]
+                + [(n, C.c_int64) for n in ("rows", "x_stride", "w_stride", "residual_stride", "y_stride")]
+                + [(n, C.c_int32) for n in ("k", "n", "dtype", "bias_dtype", "out_dtype", "activation")]
+                + [("scale", C.c_float)])
+
+
+class wfst_loglikes_args(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("x", "w", "bias", "log_prior", "lengths", "out")]
+                + [(n, C.c_int64) for n in ("x_seq_stride", "x_stride", "w_stride", "out_seq_stride", "out_stride")]
+                + [(n, C.c_int32) for n in ("seqs", "frames", "k", "v", "dtype", "bias_dtype", "out_dtype")])
+
+
+class wfst_token_logprobs_args(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("scores", "tokens", "lengths", "logprobs", "lse", "entropy", "stats", "top_ids",
+                                           "top_logprobs", "workspace")]
+                + [(n, C.c_int64) for n in ("workspace_bytes", "seq_stride", "stride")]
+                + [(n, C.c_int32) for n in ("seqs", "frames", "v", "given", "top", "dtype")])
+
+
+class wfst_token_logprobs_backward_args(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("scores", "tokens", "lengths", "stats", "entropy", "top_ids", "grad_logprobs",
+                                           "grad_lse", "grad_entropy", "grad_top", "grad_scores")]
+                + [(n, C.c_int64) for n in ("seq_stride", "stride", "grad_seq_stride", "grad_stride")]
+                + [(n, C.c_int32) for n in ("seqs", "frames", "v", "given", "top", "dtype")])
 
 
 LINK_DTYPE = np.dtype([("src", np.int32), ("dst", np.int32), ("ilabel", np.int32), ("olabel", np.int32),
@@ -141,8 +169,14 @@ def load_library():
     lib.wfst_get_lattice.argtypes = [p, i32, p, f32, p, p, i64, p, p, i64, p, p, p]
     lib.wfst_get_lattice_noalloc.argtypes = lib.wfst_get_lattice.argtypes
     lib.wfst_get_lattice_batch.argtypes = [p, p, i32, p, i32, f32, p, p, i64, p, p, i64, p, p, p]
+    lib.wfst_linear.argtypes = [C.POINTER(wfst_linear_args), p]
+    lib.wfst_loglikes.argtypes = [C.POINTER(wfst_loglikes_args), p]
+    lib.wfst_token_logprobs.argtypes = [C.POINTER(wfst_token_logprobs_args), p]
+    lib.wfst_token_logprobs_backward.argtypes = [C.POINTER(wfst_token_logprobs_backward_args), p]
+    lib.wfst_token_logprobs_workspace.argtypes = [i64, i32, i32]
+    lib.wfst_token_logprobs_workspace.restype = i64
     for name in EXPORTS:
-        if name not in ("wfst_device_bytes", "wfst_last_kernel_ms", "wfst_slot_kernel_ms", "wfst_last_error"):
+        if name not in ("wfst_token_logprobs_workspace", "wfst_device_bytes", "wfst_last_kernel_ms", "wfst_slot_kernel_ms", "wfst_last_error"):
             getattr(lib, name).restype = i32
     _lib = lib
     return lib
@@ -386,6 +420,45 @@ class Decoder:
                                                     ptr(out[0]), ptr(out[1]), ptr(out[2]), ptr(out[3]),
                                                     _stream_ptr(stream)))
         return out
+
+    # ---- from hidden states: the output layer (outputs.loglikes) in front of the decoder, on one stream
+    def _loglikes(self, hidden, weight, bias, log_prior, lengths, loglikes, stream):
+        """lengths: host int32.  Returns the [n, frames, V] tensor that the kernel fills up to each length."""
+        import torch
+        from .outputs import loglikes as output_layer
+        if hidden.dim() != 3 or weight.shape[0] != self.V:
+            raise ValueError(f"hidden {tuple(hidden.shape)} must have three dimensions and weight {tuple(weight.shape)} {self.V} rows")
+        if len(lengths) != hidden.shape[0] or (len(lengths) and not (0 <= lengths.min() and lengths.max() <= hidden.shape[1])):
+            raise ValueError("lengths must have an entry between 0 and the number of frames for every row of hidden")
+        with _on(stream):
+            if len(lengths) and lengths.min() == hidden.shape[1]:
+                dev_lengths = None                       # every frame of every row
+            else:
+                if torch.cuda.is_current_stream_capturing():
+                    raise ValueError("lengths that differ from the number of frames cannot be copied to the GPU in a graph: "
+                                     "call loglikes with lengths that are there, and decode its result")
+                host = torch.empty(len(lengths), dtype=torch.int32, pin_memory=True)
+                host.numpy()[:] = lengths
+                dev_lengths = host.to(hidden.device, non_blocking=True)
+            if loglikes is None:                         # (the decoder never reads behind a length: nothing to clear)
+                loglikes = torch.empty((*hidden.shape[:2], self.V), dtype=getattr(torch, self.loglike_dtype), device=hidden.device)
+        return output_layer(hidden, weight, bias, log_prior=log_prior, lengths=dev_lengths, out=loglikes, stream=stream)
+
+    def decode_hidden(self, hidden, lengths, weight, bias, beam, max_active, log_prior=None, loglikes=None, stream=None, **kw):
+        """decode_batch of loglikes(hidden, weight, bias, log_prior): hidden: CUDA tensor [B, T, k] of an encoder (any
+        strides of B and T); weight [V, k], bias [V] or None: its output layer; lengths: int32 host array [B].
+        loglikes: a contiguous [B, T, V] tensor of the decoder's type to keep them in (get_lattice needs them); only frames
+        before a length are written.  Other arguments and the results as in decode_batch."""
+        lengths = np.ascontiguousarray(lengths, dtype=np.int32)
+        ll = self._loglikes(hidden, weight, bias, log_prior, lengths, loglikes, stream)
+        return self.decode_batch(ll, lengths, beam, max_active, stream=stream, **kw)
+
+    def advance_hidden_partial(self, channels, hidden, nframes, weight, bias, log_prior=None, finalize=False, loglikes=None,
+                               stream=None, out=None):
+        """advance_chunk_partial of loglikes(hidden, weight, bias, log_prior): hidden [n, C, k], nframes host int32 [n]."""
+        nframes = np.ascontiguousarray(nframes, dtype=np.int32)
+        ll = self._loglikes(hidden, weight, bias, log_prior, nframes, loglikes, stream)
+        return self.advance_chunk_partial(channels, ll, nframes, finalize=finalize, stream=stream, out=out)
 
     def get_lattice_noalloc(self, ch, loglikes, lattice_beam, tok_state, tok_cost, links, frame_off, stream=None):
         """wfst_get_lattice_noalloc: every buffer is the caller's (tok_state int32 / tok_cost float32

@@ -72,6 +72,7 @@
 #include <vector>
 
 #include "wfst_decoder.h"
+#include "wfst_error.h"
 
 namespace {
 
@@ -2356,7 +2357,7 @@ struct wfst_decoder {
 };
 
 namespace {
-std::string g_create_err;
+thread_local std::string g_create_err;    // of creations and of calls without a decoder
 
 #define HIP_TRY(dec, expr)                                                              \
   do {                                                                                  \
@@ -3709,3 +3710,8 @@ float wfst_slot_kernel_ms(wfst_decoder *d, int32_t slot) {
 const char *wfst_last_error(const wfst_decoder *d) { return d ? d->err.c_str() : g_create_err.c_str(); }
 
 }  // extern "C"
+
+int wfst_note_error(int code, const char *msg) noexcept {
+  try { g_create_err = msg; } catch (...) { g_create_err.clear(); }
+  return code;
+}

@@ -1,0 +1,209 @@
+// The operators beside the decoder (the second part of include/wfst_decoder.h): checks of arguments and launches.
+#include <hip/hip_runtime.h>
+
+#include <climits>
+#include <cstdint>
+#include <cstdio>
+
+#include "wfst_decoder.h"
+#include "wfst_error.h"
+#include "wfst_linear.h"
+#include "wfst_logprobs.h"
+
+namespace {
+
+using namespace wfst_ops;
+
+int refuse(const char *what, const char *why) {
+  char msg[256];
+  snprintf(msg, sizeof msg, "%s: %s", what, why);
+  return wfst_note_error(WFST_ERR_INVALID_ARG, msg);
+}
+
+// hipLaunchKernel's own answer: an error that an earlier call of the program left behind is not taken for this one's
+template <class Args>
+int launch(const char *what, void (*kernel)(Args), int64_t workgroups, int threads, const Args &a, void *stream) {
+  if (workgroups <= 0) return WFST_OK;
+  if (workgroups > INT_MAX) return refuse(what, "too many rows for one launch");
+  Args copy = a;
+  void *argv[] = {&copy};
+  const hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)workgroups), dim3(threads), argv, 0,
+                                       static_cast<hipStream_t>(stream));
+  if (e == hipSuccess) return WFST_OK;
+  (void)hipGetLastError();
+  char msg[256];
+  snprintf(msg, sizeof msg, "%s: launch failed: %s", what, hipGetErrorString(e));
+  return wfst_note_error(WFST_ERR_HIP, msg);
+}
+
+// kernel<element type> of a template by the run-time type
+#define BY_TYPE(dtype, kernel) ((dtype) == 0 ? kernel<F32> : (dtype) == 1 ? kernel<F16> : kernel<BF16>)
+
+bool type_ok(int32_t t) { return t >= 0 && t <= 2; }
+int64_t type_size(int32_t t) { return t == 0 ? 4 : 2; }
+bool aligned(const void *p, int64_t to) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)to == 0; }
+
+// The bytes that rows (s, t) of `cols` elements take up, -1 if that does not fit 2^62.
+int64_t span(int64_t seqs, int64_t frames, int64_t cols, int64_t seq_stride, int64_t stride, int64_t size) {
+  if (seqs == 0 || frames == 0) return 0;
+  const __int128 n = ((__int128)(seqs - 1) * seq_stride + (__int128)(frames - 1) * stride + cols) * size;
+  return n > ((__int128)1 << 62) ? -1 : (int64_t)n;
+}
+
+bool overlap(const void *p, int64_t np, const void *q, int64_t nq) {
+  if (!p || !q || np <= 0 || nq <= 0) return false;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a < b + (uintptr_t)nq && b < a + (uintptr_t)np;
+}
+
+// Rows (s, t) of `cols` written elements: no two of them share one.
+bool rows_apart(int64_t seqs, int64_t frames, int64_t cols, int64_t seq_stride, int64_t stride) {
+  if (seq_stride < 0 || stride < 0) return false;
+  if (frames > 1 && stride < cols) return false;
+  if (seqs > 1 && seq_stride < cols) return false;
+  if (seqs <= 1 || frames <= 1) return true;
+  return (__int128)seq_stride >= (__int128)(frames - 1) * stride + cols || (__int128)stride >= (__int128)(seqs - 1) * seq_stride + cols;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t wfst_linear(const wfst_linear_args *args, void *stream) {
+  const char *me = "wfst_linear";
+  if (!args) return refuse(me, "null argument");
+  const wfst_linear_args &p = *args;
+  if (!type_ok(p.dtype) || !type_ok(p.out_dtype) || (p.bias && !type_ok(p.bias_dtype))) return refuse(me, "unknown element type");
+  if (p.activation < WFST_ACT_NONE || p.activation > WFST_ACT_GELU) return refuse(me, "unknown activation");
+  if (p.rows < 0 || p.k < 1 || p.n < 1) return refuse(me, "rows must be >= 0, k and n >= 1");
+  if (p.rows == 0) return WFST_OK;
+  if (!p.x || !p.w || !p.y) return refuse(me, "null x, w or y");
+  if (p.x_stride < 0 || p.w_stride < 0) return refuse(me, "negative stride");
+  if (!rows_apart(1, p.rows, p.n, 0, p.y_stride) || (p.residual && p.rows > 1 && p.residual_stride < p.n))
+    return refuse(me, "y_stride and residual_stride must be >= n");
+  const int64_t size = type_size(p.dtype), out_size = type_size(p.out_dtype);
+  if (!aligned(p.x, size) || !aligned(p.w, size) || !aligned(p.y, out_size) || !aligned(p.residual, out_size) ||
+      (p.bias && !aligned(p.bias, type_size(p.bias_dtype))))
+    return refuse(me, "an address is not a multiple of its element's size");
+  const int64_t nx = span(1, p.rows, p.k, 0, p.x_stride, size), nw = span(1, p.n, p.k, 0, p.w_stride, size);
+  const int64_t ny = span(1, p.rows, p.n, 0, p.y_stride, out_size), nr = p.residual ? span(1, p.rows, p.n, 0, p.residual_stride, out_size) : 0;
+  if (nx < 0 || nw < 0 || ny < 0 || nr < 0) return refuse(me, "sizes and strides are too large");
+  if (overlap(p.y, ny, p.x, nx) || overlap(p.y, ny, p.w, nw) || (p.bias && overlap(p.y, ny, p.bias, p.n * type_size(p.bias_dtype))))
+    return refuse(me, "y overlaps what is read");
+  if (overlap(p.y, ny, p.residual, nr) && !(p.residual == p.y && (p.residual_stride == p.y_stride || p.rows == 1)))
+    return refuse(me, "y overlaps the residual without being it");
+  LinearArgs a{p.x, p.w, p.bias, p.residual, p.y, p.rows, p.x_stride, p.w_stride, p.residual_stride, p.y_stride,
+               p.k, p.n, p.bias_dtype, p.out_dtype, p.activation, p.scale};
+  const int64_t tiles_m = (p.rows - 1) / 64 + 1, tiles_n = ((int64_t)p.n - 1) / 64 + 1;
+  if (tiles_m > INT_MAX / tiles_n) return refuse(me, "too many rows for one launch");
+  return launch(me, BY_TYPE(p.dtype, linear_kernel), tiles_m * tiles_n, 256, a, stream);
+}
+
+int32_t wfst_loglikes(const wfst_loglikes_args *args, void *stream) {
+  const char *me = "wfst_loglikes";
+  if (!args) return refuse(me, "null argument");
+  const wfst_loglikes_args &p = *args;
+  if (!type_ok(p.dtype) || !type_ok(p.out_dtype) || (p.bias && !type_ok(p.bias_dtype))) return refuse(me, "unknown element type");
+  if (p.seqs < 0 || p.frames < 0 || p.k < 1) return refuse(me, "seqs and frames must be >= 0, k >= 1");
+  if (p.v < 1 || p.v > 2048) return refuse(me, "v must be 1 to 2048");
+  if (p.seqs == 0 || p.frames == 0) return WFST_OK;
+  if (!p.x || !p.w || !p.out) return refuse(me, "null x, w or out");
+  if (p.x_seq_stride < 0 || p.x_stride < 0 || p.w_stride < 0) return refuse(me, "negative stride");
+  if (!rows_apart(p.seqs, p.frames, p.v, p.out_seq_stride, p.out_stride)) return refuse(me, "the rows of out overlap");
+  const int64_t size = type_size(p.dtype), out_size = type_size(p.out_dtype);
+  if (!aligned(p.x, size) || !aligned(p.w, size) || !aligned(p.out, out_size) || !aligned(p.log_prior, 4) || !aligned(p.lengths, 4) ||
+      (p.bias && !aligned(p.bias, type_size(p.bias_dtype))))
+    return refuse(me, "an address is not a multiple of its element's size");
+  const int64_t nx = span(p.seqs, p.frames, p.k, p.x_seq_stride, p.x_stride, size), nw = span(1, p.v, p.k, 0, p.w_stride, size);
+  const int64_t no = span(p.seqs, p.frames, p.v, p.out_seq_stride, p.out_stride, out_size);
+  if (nx < 0 || nw < 0 || no < 0) return refuse(me, "sizes and strides are too large");
+  if (overlap(p.out, no, p.x, nx) || overlap(p.out, no, p.w, nw) || (p.bias && overlap(p.out, no, p.bias, p.v * type_size(p.bias_dtype))) ||
+      overlap(p.out, no, p.log_prior, (int64_t)p.v * 4) || overlap(p.out, no, p.lengths, (int64_t)p.seqs * 4))
+    return refuse(me, "out overlaps what is read");
+  LoglikesArgs a{p.x, p.w, p.bias, p.log_prior, p.lengths, p.out, p.x_seq_stride, p.x_stride, p.w_stride, p.out_seq_stride, p.out_stride,
+                 p.seqs, p.frames, p.k, p.v, p.bias_dtype, p.out_dtype};
+  return launch(me, BY_TYPE(p.dtype, loglikes_kernel), (int64_t)p.seqs * p.frames, 256, a, stream);
+}
+
+int64_t wfst_token_logprobs_workspace(int64_t, int32_t, int32_t) { return 0; }
+
+int32_t wfst_token_logprobs(const wfst_token_logprobs_args *args, void *stream) {
+  const char *me = "wfst_token_logprobs";
+  if (!args) return refuse(me, "null argument");
+  const wfst_token_logprobs_args &p = *args;
+  if (!type_ok(p.dtype)) return refuse(me, "unknown element type");
+  if (p.seqs < 0 || p.frames < 0) return refuse(me, "seqs and frames must be >= 0");
+  if (p.v < 1 || p.v > (1 << 30)) return refuse(me, "v must be 1 to 2^30");
+  if (p.given < 0 || p.given > 4096) return refuse(me, "given must be 0 to 4096");
+  if (p.top < 0 || p.top > 64 || p.top > p.v) return refuse(me, "top must be 0 to 64, and at most v");
+  if (p.seqs == 0 || p.frames == 0) return WFST_OK;
+  if (!p.scores || (p.given && p.logprobs && !p.tokens)) return refuse(me, "null scores or tokens");
+  if (p.seq_stride < 0 || p.stride < 0) return refuse(me, "negative stride");
+  const int64_t size = type_size(p.dtype), rows = (int64_t)p.seqs * p.frames;
+  if (rows > INT_MAX) return refuse(me, "more than 2^31 - 1 rows");
+  if (!aligned(p.scores, size) || !aligned(p.tokens, 4) || !aligned(p.lengths, 4) || !aligned(p.logprobs, 4) || !aligned(p.lse, 4) ||
+      !aligned(p.entropy, 4) || !aligned(p.stats, 4) || !aligned(p.top_ids, 4) || !aligned(p.top_logprobs, 4))
+    return refuse(me, "an address is not a multiple of its element's size");
+  const int64_t need = wfst_token_logprobs_workspace(rows, p.v, p.top);
+  if (need > 0 && (!p.workspace || p.workspace_bytes < need || !aligned(p.workspace, 16)))
+    return refuse(me, "the workspace is missing, too small or not 16-byte aligned");
+  const int64_t ns = span(p.seqs, p.frames, p.v, p.seq_stride, p.stride, size);
+  if (ns < 0) return refuse(me, "sizes and strides are too large");
+  struct Part { const void *p; int64_t n; };
+  const Part read[] = {{p.scores, ns}, {p.tokens, rows * p.given * 4}, {p.lengths, (int64_t)p.seqs * 4}};
+  const Part wrote[] = {{p.given ? p.logprobs : nullptr, rows * p.given * 4}, {p.lse, rows * 4}, {p.entropy, rows * 4}, {p.stats, rows * 8},
+                        {p.top ? p.top_ids : nullptr, rows * p.top * 4}, {p.top ? p.top_logprobs : nullptr, rows * p.top * 4},
+                        {p.workspace, need}};
+  for (int i = 0; i < 7; ++i) {
+    for (const Part &r : read)
+      if (overlap(wrote[i].p, wrote[i].n, r.p, r.n)) return refuse(me, "an output overlaps what is read");
+    for (int j = 0; j < i; ++j)
+      if (overlap(wrote[i].p, wrote[i].n, wrote[j].p, wrote[j].n)) return refuse(me, "two outputs overlap");
+  }
+  LogprobsArgs a{p.scores, p.tokens, p.lengths, p.given ? p.logprobs : nullptr, p.lse, p.entropy, p.stats, p.top ? p.top_ids : nullptr,
+                 p.top ? p.top_logprobs : nullptr, p.seq_stride, p.stride, p.seqs, p.frames, p.v, p.given, p.top};
+  if (!a.top_ids && !a.top_logprobs) a.top = 0;
+  return launch(me, BY_TYPE(p.dtype, logprobs_kernel), rows, 256, a, stream);
+}
+
+int32_t wfst_token_logprobs_backward(const wfst_token_logprobs_backward_args *args, void *stream) {
+  const char *me = "wfst_token_logprobs_backward";
+  if (!args) return refuse(me, "null argument");
+  const wfst_token_logprobs_backward_args &p = *args;
+  if (!type_ok(p.dtype)) return refuse(me, "unknown element type");
+  if (p.seqs < 0 || p.frames < 0) return refuse(me, "seqs and frames must be >= 0");
+  if (p.v < 1 || p.v > (1 << 30)) return refuse(me, "v must be 1 to 2^30");
+  if (p.given < 0 || p.given > 4096) return refuse(me, "given must be 0 to 4096");
+  if (p.top < 0 || p.top > 64 || p.top > p.v) return refuse(me, "top must be 0 to 64, and at most v");
+  if (p.seqs == 0 || p.frames == 0) return WFST_OK;
+  if (!p.scores || !p.stats || !p.grad_scores) return refuse(me, "null scores, stats or grad_scores");
+  if (p.given && p.grad_logprobs && !p.tokens) return refuse(me, "grad_logprobs without tokens");
+  if (p.grad_entropy && !p.entropy) return refuse(me, "grad_entropy without entropy");
+  if (p.top && p.grad_top && !p.top_ids) return refuse(me, "grad_top without top_ids");
+  if (p.seq_stride < 0 || p.stride < 0) return refuse(me, "negative stride");
+  if (!rows_apart(p.seqs, p.frames, p.v, p.grad_seq_stride, p.grad_stride)) return refuse(me, "the rows of grad_scores overlap");
+  const int64_t size = type_size(p.dtype), rows = (int64_t)p.seqs * p.frames;
+  if (rows > INT_MAX) return refuse(me, "more than 2^31 - 1 rows");
+  if (!aligned(p.scores, size) || !aligned(p.grad_scores, size) || !aligned(p.tokens, 4) || !aligned(p.lengths, 4) || !aligned(p.stats, 4) ||
+      !aligned(p.entropy, 4) || !aligned(p.top_ids, 4) || !aligned(p.grad_logprobs, 4) || !aligned(p.grad_lse, 4) ||
+      !aligned(p.grad_entropy, 4) || !aligned(p.grad_top, 4))
+    return refuse(me, "an address is not a multiple of its element's size");
+  const int64_t ns = span(p.seqs, p.frames, p.v, p.seq_stride, p.stride, size);
+  const int64_t ng = span(p.seqs, p.frames, p.v, p.grad_seq_stride, p.grad_stride, size);
+  if (ns < 0 || ng < 0) return refuse(me, "sizes and strides are too large");
+  const bool same = p.scores == p.grad_scores && (p.seqs == 1 || p.seq_stride == p.grad_seq_stride) && (p.frames == 1 || p.stride == p.grad_stride);
+  if (!same && overlap(p.grad_scores, ng, p.scores, ns)) return refuse(me, "grad_scores overlaps the scores without being them");
+  if (overlap(p.grad_scores, ng, p.tokens, rows * p.given * 4) || overlap(p.grad_scores, ng, p.lengths, (int64_t)p.seqs * 4) ||
+      overlap(p.grad_scores, ng, p.stats, rows * 8) || overlap(p.grad_scores, ng, p.entropy, rows * 4) ||
+      overlap(p.grad_scores, ng, p.top_ids, rows * p.top * 4) || overlap(p.grad_scores, ng, p.grad_logprobs, rows * p.given * 4) ||
+      overlap(p.grad_scores, ng, p.grad_lse, rows * 4) || overlap(p.grad_scores, ng, p.grad_entropy, rows * 4) ||
+      overlap(p.grad_scores, ng, p.grad_top, rows * p.top * 4))
+    return refuse(me, "grad_scores overlaps what is read");
+  BackwardArgs a{p.scores, p.tokens, p.lengths, p.stats, p.entropy, p.top_ids, p.grad_logprobs, p.grad_lse, p.grad_entropy, p.grad_top,
+                 p.grad_scores, p.seq_stride, p.stride, p.grad_seq_stride, p.grad_stride, p.seqs, p.frames, p.v, p.given, p.top};
+  if (!a.grad_logprobs) a.given = 0;
+  if (!a.grad_top) a.top = 0;
+  return launch(me, BY_TYPE(p.dtype, logprobs_backward_kernel), rows, 256, a, stream);
+}
+
+}  // extern "C"

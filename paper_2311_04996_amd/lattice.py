@@ -1,7 +1,8 @@
 """Host-side view of a lattice returned by wfst_get_lattice, and n-best paths through it.
 
 The links are found on the GPU; what is here is bookkeeping over the returned arrays (numpy,
-plain Python), for callers that want paths rather than links.
+plain Python), for callers that want paths rather than links, and the call that tells how sure
+the model was of a path's labels.
 """
 from __future__ import annotations
 
@@ -88,3 +89,28 @@ class Lattice:
                 if np.isfinite(togo[d]):
                     heapq.heappush(heap, (g + inc[k] + togo[d], g + inc[k], d, path + (k,)))
         return out
+
+    def frame_labels(self, links) -> np.ndarray:
+        """The class (column of the log-likelihoods) that a path, a list of link indices as nbest gives it, takes in
+        every frame: int32 [num_frames], -1 in a frame that the path does not cross."""
+        out = np.full(self.num_frames, -1, np.int32)
+        k = self.links[np.asarray(links, dtype=np.int64)]
+        k = k[k["ilabel"] > 0]                   # an emitting link into A_t has read row t - 1
+        out[k["frame"] - 1] = k["ilabel"] - 1
+        return out
+
+    def path_logprobs(self, scores, paths, top=0, stream=None):
+        """How sure the model was of the labels of n paths, frame by frame: token_logprobs of scores (CUDA [num_frames,
+        V], the model's logits or log-likelihoods) at the paths' labels: logprobs [num_frames, n], and of every frame lse,
+        entropy and the `top` best labels.  paths: lists of link indices, as nbest gives them."""
+        import torch
+        from .binding import _on
+        from .outputs import token_logprobs
+        if scores.dim() != 2 or scores.shape[0] != self.num_frames:
+            raise ValueError(f"scores {tuple(scores.shape)} must have {self.num_frames} rows")
+        labels = np.stack([self.frame_labels(p) for p in paths], axis=1) if len(paths) else np.zeros((self.num_frames, 0), np.int32)
+        if labels.size and int(labels.max()) >= scores.shape[1]:
+            raise ValueError(f"a path's label is beyond the {scores.shape[1]} classes of the scores")
+        with _on(stream):
+            tokens = torch.from_numpy(labels).to(scores.device)
+        return token_logprobs(scores, tokens, top=top, stream=stream)
