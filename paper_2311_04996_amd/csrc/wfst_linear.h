@@ -7,55 +7,442 @@
 
 namespace wfst_ops {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
 struct LinearArgs {
   const void *x, *w, *bias, *residual;
   void *y;
   int64_t rows, x_stride, w_stride, residual_stride, y_stride;
   int32_t k, n, bias_dtype, out_dtype, activation;
   float scale;
+  int32_t tiles_n;               // tiles along n; the grid has tiles_n times the tiles along the rows
 };
 
 // relu, silu and gelu as the header defines them; a NaN stays one
 __device__ __forceinline__ float activate(float z, int act) {
   if (act == 1) return z < 0.0f ? 0.0f : z;
-  if (act == 2) return z / (1.0f + exp_fast(-z));
+  if (act == 2) return z * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));   // (the hardware's 1 / x is within 1 ulp)
   if (act == 3) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
   return z;
 }
 
-// 64 x 64 results per workgroup of 256, 4 x 4 per lane, 16 columns of x and w at a time through LDS
-template <class E>
-__global__ __launch_bounds__(256) void linear_kernel(LinearArgs a) {
-  __shared__ float xs[16][65], ws[16][65];
-  const typename E::T *x = static_cast<const typename E::T *>(a.x), *w = static_cast<const typename E::T *>(a.w);
-  const int tiles_n = (a.n + 63) / 64;
-  const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * 64;
-  const int n0 = (int)(blockIdx.x % tiles_n) * 64;
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < a.k; k0 += 16) {
-    for (int i = threadIdx.x; i < 64 * 16; i += 256) {
-      const int r = i / 16, c = i % 16;
-      xs[c][r] = m0 + r < a.rows && k0 + c < a.k ? E::get(x[(m0 + r) * a.x_stride + k0 + c]) : 0.0f;
-      ws[c][r] = n0 + r < a.n && k0 + c < a.k ? E::get(w[(n0 + r) * a.w_stride + k0 + c]) : 0.0f;
-    }
-    __syncthreads();
-    for (int c = 0; c < 16; ++c)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_fmaf(xs[c][ty + 16 * i], ws[c][tx + 16 * j], acc[i][j]);
-    __syncthreads();
+// 8 values to or from 8 neighbouring elements (a 16-byte access may start at any of them), or the first `count` < 8 one by one
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef bf16x8 bf16x8_any __attribute__((aligned(2)));
+typedef f16x8 f16x8_any __attribute__((aligned(2)));
+__device__ __forceinline__ void load8(const void *p, int64_t i, int dtype, int count, float (&v)[8]) {
+  if (count < 8) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < count ? load_as(p, i + e, dtype) : 0.0f;
+  } else if (dtype == 0) {
+    const f32x4_any *q = reinterpret_cast<const f32x4_any *>(static_cast<const float *>(p) + i);
+    const f32x4 lo = q[0], hi = q[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = lo[e]; v[4 + e] = hi[e]; }
+  } else if (dtype == 1) {
+    const f16x8 h = *reinterpret_cast<const f16x8_any *>(static_cast<const _Float16 *>(p) + i);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
+  } else {
+    const bf16x8 h = *reinterpret_cast<const bf16x8_any *>(static_cast<const __bf16 *>(p) + i);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t m = m0 + ty + 16 * i;
-      const int n = n0 + tx + 16 * j;
-      if (m >= a.rows || n >= a.n) continue;
-      float z = acc[i][j];
-      if (a.bias) z += load_as(a.bias, n, a.bias_dtype);
-      z = a.scale * activate(z, a.activation);
-      if (a.residual) z += load_as(a.residual, m * a.residual_stride + n, a.out_dtype);
-      store_as(a.y, m * a.y_stride + n, a.out_dtype, z);
+}
+// (Stored past the caches, as streams: tiles written through them leave in no order, which the memory pays for.  118,417 x 2,048
+// results of 16 bits: 409 us for the whole product by way of the caches, 331 past them; never slower, down to the smallest calls.)
+__device__ __forceinline__ void store8(void *p, int64_t i, int dtype, int count, const float (&v)[8]) {
+  if (count < 8) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < count) store_as(p, i + e, dtype, v[e]);
+  } else if (dtype == 0) {
+    f32x4_any *q = reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + i);
+    __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, q);
+    __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, q + 1);
+  } else if (dtype == 1) {
+    f16x8 h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = (_Float16)v[e];
+    __builtin_nontemporal_store(h, reinterpret_cast<f16x8_any *>(static_cast<_Float16 *>(p) + i));
+  } else {
+    bf16x8 h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = (__bf16)v[e];
+    __builtin_nontemporal_store(h, reinterpret_cast<bf16x8_any *>(static_cast<__bf16 *>(p) + i));
+  }
+}
+
+// what follows the product sums v of columns col.. of row m
+__device__ __forceinline__ void finish(const LinearArgs &a, int64_t m, int col, float (&v)[8], const float (&bias)[8]) {
+  const int count = a.n - col;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] += bias[e];
+  if (a.activation == 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = activate(v[e], 1);
+  } else if (a.activation == 2) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = activate(v[e], 2);
+  } else if (a.activation == 3) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = activate(v[e], 3);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+  if (a.residual) {
+    float r[8];
+    load8(a.residual, m * a.residual_stride + col, a.out_dtype, count, r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += r[e];
+  }
+  store8(a.y, m * a.y_stride + col, a.out_dtype, count, v);
+}
+
+// ---- the product of a tile
+//
+// A matrix instruction takes 16-byte chunks: a lane holds one chunk (8 elements of 16 bits, 4 of 32) of a row of w and one of a row of
+// x, and gets 16 of the 32 x 32 sums.  w is the first operand, so that the sums of a lane are of ONE row of x (lane % 32) and
+// of 4 neighbouring columns each (of 8 i + 4 (lane / 32), i = 0..3): results leave 16 bytes at a time, and a softmax
+// over the columns stays in the lane but for one exchange with lane ^ 32.
+template <class E> struct Mma {                        // 16 elements of k per step
+  static __device__ __forceinline__ f32x16 run(i32x4 w, i32x4 x, f32x16 c);
+};
+template <> __device__ __forceinline__ f32x16 Mma<BF16>::run(i32x4 w, i32x4 x, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x16 Mma<F16>::run(i32x4 w, i32x4 x, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, x), c, 0, 0, 0);
+}
+// fp32: the instruction takes one element of k per half wave.  Which one is free, as long as w and x agree: element i of the chunk.
+template <> __device__ __forceinline__ f32x16 Mma<F32>::run(i32x4 w, i32x4 x, f32x16 c) {
+  const f32x4 a = __builtin_bit_cast(f32x4, w), b = __builtin_bit_cast(f32x4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+  return c;
+}
+
+template <int N> __device__ __forceinline__ void wait_loads() {       // at most N vector loads are still on their way
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
+}
+// all LDS reads of this wave are done, then all waves' are
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);                                  // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// A range of memory whose accesses are held against its end; what is behind that is not read.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer(const void *p, uint32_t bytes) {
+  // (word 3 of the descriptor: data format "32 bits", no swizzling)
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
+}
+// from the first of `rows` rows on to the end of the last one, at most what an offset of 32 bits reaches
+__device__ __forceinline__ uint32_t bytes_behind(int64_t rows, int64_t stride, int k, int size) {
+  const int64_t n = ((rows - 1) * stride + k) * size;
+  return n < 0xfffffff0ll ? (uint32_t)n : 0xfffffff0u;
+}
+
+// 16 bytes from byte `off` of a row of k_bytes, zero behind its end
+template <class E> __device__ __forceinline__ i32x4 chunk_of(const char *row, int64_t off, int64_t k_bytes) {
+  constexpr int kSize = (int)sizeof(typename E::T);
+  i32x4 c = {0, 0, 0, 0};
+  if (off + 16 <= k_bytes) {
+    __builtin_memcpy(&c, __builtin_assume_aligned(row + off, kSize), 16);
+  } else if (off < k_bytes) {
+    typename E::T e[16 / kSize];
+#pragma unroll
+    for (int i = 0; i < 16 / kSize; ++i)
+      e[i] = off + i * kSize < k_bytes ? reinterpret_cast<const typename E::T *>(row + off)[i] : (typename E::T)0.0f;
+    __builtin_memcpy(&c, e, 16);
+  }
+  return c;
+}
+
+// A tile of BM rows of x by BN rows of w, WM x WN of them per wave.  LDS holds kStages parts of kRow bytes of k of each row, at
+// chunk c ^ swizzle(row): the 16 lanes that read a column of chunks together are then in different banks.
+template <class E, int BM, int BN, int WM, int WN, int ROW>
+struct Tile {
+  static constexpr int kWavesM = BM / WM, kWavesN = BN / WN, kWaves = kWavesM * kWavesN, kThreads = 64 * kWaves;
+  static constexpr int kRow = ROW, kChunks = ROW / 16;
+  static constexpr int kStage = (BM + BN) * ROW, kStages = 3;
+  static constexpr int kLoads = kStage / 1024 / kWaves;                // 1024 bytes per wave and load
+  static constexpr int kTM = WM / 32, kTN = WN / 32;
+  static_assert(kStage % (1024 * kWaves) == 0 && WM % 32 == 0 && WN % 32 == 0 && (ROW == 64 || ROW == 128), "whole loads per wave");
+
+  static __device__ __forceinline__ int swizzle(int row) { return ROW == 64 ? (row >> 2) & 3 : (row >> 1) & 7; }
+
+  // Piece i of this wave: 1024 bytes of a stage, 64 / kChunks rows of it.  Row r of the tile is x's row r for r < BM, w's row r - BM behind
+  // that; a piece is of one of them.
+  static __device__ __forceinline__ int piece(int i) { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) + kWaves * i; }
+  static __device__ __forceinline__ int piece_row(int i) { return piece(i) * (64 / kChunks) + (threadIdx.x & 63) / kChunks; }
+  static __device__ __forceinline__ int piece_chunk(int i) { return ((threadIdx.x & 63) % kChunks) ^ swizzle(piece_row(i)); }
+
+  // Where this lane's chunks of the pieces lie behind the start of x or w, in bytes.
+  int at[kLoads];
+  // offset_of(r): of row r of the tile.  A row behind the end may be any other one, or lie out of bounds
+  template <class OffsetOf> __device__ __forceinline__ void aim(OffsetOf offset_of) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) at[i] = offset_of(piece_row(i)) + piece_chunk(i) * 16;
+  }
+  // Part `part` of k on its way into `stage`, without a register between.  Chunks behind the end of a row are whatever lies
+  // there, or nothing if that is out of bounds: they are put to zero where they are used.
+  __device__ __forceinline__ void load(Buffer x, Buffer w, char *stage, int part) const {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(piece(i) * (64 / kChunks) < BM ? x : w,
+                                               (__attribute__((address_space(3))) void *)(stage + piece(i) * 1024), 16, at[i], part * ROW, 0, 0);
+  }
+  // The same by way of registers, for rows whose chunks are no multiples of 16 bytes in memory (a 16-byte load may start
+  // anywhere) or end inside one; what is behind the end of a row is zero.
+  static __device__ __forceinline__ void fetch(i32x4 (&reg)[kLoads], const char *const (&from)[kLoads], int part, int k_bytes) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) reg[i] = chunk_of<E>(from[i], part * ROW + piece_chunk(i) * 16, k_bytes);
+  }
+  static __device__ __forceinline__ void put(char *stage, const i32x4 (&reg)[kLoads]) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<i32x4 *>(stage + piece(i) * 1024 + (threadIdx.x & 63) * 16) = reg[i];
+  }
+  // What a wave multiplies in one step: 16 bytes of k per lane, half of the wave each of two neighbouring chunks.
+  struct Step { i32x4 w[kTN], x[kTM]; };
+  static constexpr int kSteps = kChunks / 2;
+  static __device__ __forceinline__ void read(Step &f, const char *stage, int step) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = 2 * step + (lane >> 5);
+    const int m0 = (wave / kWavesN) * WM + (lane & 31), n0 = BM + (wave % kWavesN) * WN + (lane & 31);
+#pragma unroll
+    for (int i = 0; i < kTN; ++i) f.w[i] = *reinterpret_cast<const i32x4 *>(stage + (n0 + 32 * i) * ROW + (q ^ swizzle(n0 + 32 * i)) * 16);
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) f.x[i] = *reinterpret_cast<const i32x4 *>(stage + (m0 + 32 * i) * ROW + (q ^ swizzle(m0 + 32 * i)) * 16);
+  }
+  // acc[n][m] += the step's products.
+  static __device__ __forceinline__ void multiply(const Step &f, f32x16 (&acc)[kTN][kTM]) {
+#pragma unroll
+    for (int i = 0; i < kTN; ++i)
+#pragma unroll
+      for (int j = 0; j < kTM; ++j) acc[i][j] = Mma<E>::run(f.w[i], f.x[j], acc[i][j]);
+  }
+  // The same at the end of k, `left` bytes of which are left at the part's start: what is behind them counts as zero, in x and
+  // in w (it may be NaN in either).
+  static __device__ __forceinline__ void multiply_last(Step &f, int step, int left, f32x16 (&acc)[kTN][kTM]) {
+    if ((2 * step + ((threadIdx.x & 63) >> 5)) * 16 >= left) {
+#pragma unroll
+      for (int i = 0; i < kTN; ++i) f.w[i] = i32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < kTM; ++i) f.x[i] = i32x4{0, 0, 0, 0};
     }
+    multiply(f, acc);
+  }
+  // One part but the last, from stage `here`: the next step's chunks are read while a step is multiplied, across the parts too.
+  // Before the last step the waves meet: the part behind has arrived in `next` then, and nobody reads `here` any more, so
+  // that the part three further on can come there.
+  __device__ __forceinline__ void part(int p, Buffer x, Buffer w, char *here, char *next, Step (&f)[2], f32x16 (&acc)[kTN][kTM]) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      if (s + 1 < kSteps) {
+        read(f[(s + 1) & 1], here, s + 1);
+      } else {
+        wait_loads<kLoads>();
+        meet();
+        read(f[0], next, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        load(x, w, here, p + 3);
+      }
+      __builtin_amdgcn_sched_barrier(0);             // the reads go out before the products that hide them
+      multiply(f[s & 1], acc);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // The whole product.  Ends with all waves done with LDS.  (Three parts behind the last one are loaded too, while the last ones
+  // are multiplied, and not used: so every wait has the same number of loads behind it.)
+  __device__ __forceinline__ void product(Buffer x, Buffer w, char *s0, char *s1, char *s2, int k_bytes, f32x16 (&acc)[kTN][kTM]) {
+    const int parts = (k_bytes + ROW - 1) / ROW;
+    Step f[2];
+    load(x, w, s0, 0);
+    load(x, w, s1, 1);
+    load(x, w, s2, 2);
+    wait_loads<2 * kLoads>();
+    meet();
+    read(f[0], s0, 0);
+    int p = 0;
+    for (; p + 3 < parts; p += 3) {
+      part(p, x, w, s0, s1, f, acc);
+      part(p + 1, x, w, s1, s2, f, acc);
+      part(p + 2, x, w, s2, s0, f, acc);
+    }
+    if (p + 1 < parts) part(p, x, w, s0, s1, f, acc);
+    if (p + 2 < parts) part(p + 1, x, w, s1, s2, f, acc);
+    const char *last = p + 1 == parts ? s0 : p + 2 == parts ? s1 : s2;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      if (s + 1 < kSteps) read(f[(s + 1) & 1], last, s + 1);
+      multiply_last(f[s & 1], s, k_bytes - (parts - 1) * ROW, acc);
+    }
+    wait_loads<0>();
+    meet();
+  }
+  // row_of(r): start of row r of the tile; a row behind the end may be any other one
+  template <class RowOf>
+  static __device__ __forceinline__ void product_staged(RowOf row_of, char *s0, char *s1, int k_bytes, f32x16 (&acc)[kTN][kTM]) {
+    const int parts = (k_bytes + ROW - 1) / ROW;
+    const char *from[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) from[i] = row_of(piece_row(i));
+    i32x4 ahead[2][kLoads];                            // parts on their way: p + 1, p + 2
+    fetch(ahead[0], from, 0, k_bytes);
+    fetch(ahead[1], from, 1, k_bytes);
+    put(s0, ahead[0]);
+    meet();
+    for (int p = 0; p < parts; p += 2) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const char *here = i ? s1 : s0;
+        if (p + i >= parts) break;
+        fetch(ahead[i], from, p + i + 2, k_bytes);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          Step f;
+          read(f, here, s);
+          multiply(f, acc);
+        }
+        put(i ? s0 : s1, ahead[1 - i]);                // nobody reads there since the waves last met
+        meet();
+      }
+    }
+  }
+};
+
+// Tile `block` of the grid in an order that suits the dies: workgroup b runs on die b % 8, each of which has its own L2, and
+// gets neighbouring tiles there, along n first (they share their rows of x, and all of them w).
+__device__ __forceinline__ int64_t tile_of(int64_t block, int64_t tiles) {
+  const int64_t per = tiles / 8, more = tiles % 8, die = block % 8, i = block / 8;
+  return die * per + (die < more ? die : more) + i;
+}
+
+// DIRECT: rows of x and w start at multiples of 16 bytes and are whole chunks, and a tile's rows lie within 2 GB
+template <class E, int BM, int BN, int WM, int WN, int ROW, bool DIRECT>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_kernel(LinearArgs a) {
+  using T = Tile<E, BM, BN, WM, WN, ROW>;
+  constexpr int kPitch = WN + 4;                        // floats; 32 rows of it per wave in the epilogue
+  constexpr int kWaveOut = 32 * kPitch * 4, kPer = (T::kWaves + 2) / 3;      // waves per stage there
+  constexpr int kLds = T::kStage > kWaveOut * kPer ? T::kStage : kWaveOut * kPer;
+  __shared__ __align__(16) char s0[kLds], s1[kLds], s2[kLds];
+  const int64_t tile = tile_of(blockIdx.x, gridDim.x);
+  const int64_t m0 = tile / a.tiles_n * BM;
+  const int n0 = (int)(tile % a.tiles_n) * BN;
+  const char *x = static_cast<const char *>(a.x), *w = static_cast<const char *>(a.w);
+  constexpr int kSize = (int)sizeof(typename E::T);
+  f32x16 acc[T::kTN][T::kTM];
+#pragma unroll
+  for (int i = 0; i < T::kTN; ++i)
+#pragma unroll
+    for (int j = 0; j < T::kTM; ++j) acc[i][j] = f32x16{};
+  const char *xt = x + m0 * a.x_stride * kSize, *wt = w + (int64_t)n0 * a.w_stride * kSize;   // the tile's first rows
+  if (DIRECT) {
+    T t;
+    t.aim([&](int r) { return r < BM ? r * (int)a.x_stride * kSize : (r - BM) * (int)a.w_stride * kSize; });
+    t.product(buffer(xt, bytes_behind(a.rows - m0, a.x_stride, a.k, kSize)), buffer(wt, bytes_behind(a.n - n0, a.w_stride, a.k, kSize)), s0, s1, s2,
+              a.k * kSize, acc);
+  } else {
+    T::product_staged([&](int r) {
+      const int64_t m = m0 + r < a.rows ? r : a.rows - 1 - m0, n = n0 + (r - BM) < a.n ? r - BM : a.n - 1 - n0;
+      return r < BM ? xt + m * a.x_stride * kSize : wt + n * a.w_stride * kSize;
+    }, s0, s1, a.k * kSize, acc);
+  }
+
+  // Epilogue: 32 rows at a time go through the wave's own part of LDS, so that a lane gets 8 neighbouring columns of a row.
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float *out = reinterpret_cast<float *>((wave / kPer == 0 ? s0 : wave / kPer == 1 ? s1 : s2) + (wave % kPer) * kWaveOut);
+  const int nw = n0 + (wave % T::kWavesN) * WN;
+  const int64_t mw = m0 + (wave / T::kWavesN) * WM;
+  constexpr int kLanes = WN / 8, kRows = 64 / kLanes;   // lanes per row, rows at a time
+  const int col = nw + (lane % kLanes) * 8;
+  float bias[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bias[e] = a.bias && col + e < a.n ? load_as(a.bias, col + e, a.bias_dtype) : 0.0f;
+#pragma unroll
+  for (int j = 0; j < T::kTM; ++j) {
+#pragma unroll
+    for (int i = 0; i < T::kTN; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4 *>(out + (lane & 31) * kPitch + 32 * i + 8 * q + 4 * (lane >> 5)) =
+            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int r = 0; r < 32; r += kRows) {
+      const int64_t m = mw + 32 * j + r + lane / kLanes;
+      const float *z = out + (r + lane / kLanes) * kPitch + (lane % kLanes) * 8;
+      const f32x4 z0 = *reinterpret_cast<const f32x4 *>(z), z1 = *reinterpret_cast<const f32x4 *>(z + 4);
+      float v[8] = {z0[0], z0[1], z0[2], z0[3], z1[0], z1[1], z1[2], z1[3]};
+      if (m < a.rows && col < a.n) finish(a, m, col, v, bias);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Few rows: 16 rows of x by 16 of w per workgroup of 8 waves, which share out k (16 bytes per lane and step, 64 of a row, from
+// memory into registers: nothing is used twice, and all loads of 4 KB of a row are on their way at once) and add their sums up
+// through LDS, in the order of the waves.
+template <class E> struct MmaFew {                     // 64 bytes of k per step, a quarter of them per 16 lanes
+  static __device__ __forceinline__ f32x4 run(i32x4 w, i32x4 x, f32x4 c);
+};
+template <> __device__ __forceinline__ f32x4 MmaFew<BF16>::run(i32x4 w, i32x4 x, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x4 MmaFew<F16>::run(i32x4 w, i32x4 x, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, x), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x4 MmaFew<F32>::run(i32x4 w, i32x4 x, f32x4 c) {
+  const f32x4 a = __builtin_bit_cast(f32x4, w), b = __builtin_bit_cast(f32x4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+  return c;
+}
+
+template <class E>
+__global__ __launch_bounds__(512) void linear_few_kernel(LinearArgs a) {
+  constexpr int kWaves = 8, kSteps = 8;
+  __shared__ __align__(16) float part[kWaves][16][20];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t m0 = (int64_t)(blockIdx.x / a.tiles_n) * 16;
+  const int n0 = (int)(blockIdx.x % a.tiles_n) * 16;
+  constexpr int kSize = (int)sizeof(typename E::T);
+  const int64_t m = m0 + (lane & 15) < a.rows ? m0 + (lane & 15) : a.rows - 1;
+  const int64_t n = n0 + (lane & 15) < a.n ? n0 + (lane & 15) : a.n - 1;
+  const char *x = static_cast<const char *>(a.x) + m * a.x_stride * kSize, *w = static_cast<const char *>(a.w) + n * a.w_stride * kSize;
+  const int64_t k_bytes = (int64_t)a.k * kSize;
+  f32x4 acc = {};
+  for (int64_t at = wave * 64 + (lane >> 4) * 16; at - (lane >> 4) * 16 < k_bytes; at += kWaves * kSteps * 64) {
+    i32x4 xf[kSteps], wf[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      wf[i] = chunk_of<E>(w, at + i * (kWaves * 64), k_bytes);
+      xf[i] = chunk_of<E>(x, at + i * (kWaves * 64), k_bytes);
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) acc = MmaFew<E>::run(wf[i], xf[i], acc);
+  }
+  *reinterpret_cast<f32x4 *>(&part[wave][lane & 15][4 * (lane >> 4)]) = acc;       // a lane's 4 sums: columns 4 (lane / 16).. of row lane % 16
+  __syncthreads();
+  const int r = threadIdx.x >> 1, col = (threadIdx.x & 1) * 8;         // the first 32 threads: 8 columns each
+  if (r >= 16 || m0 + r >= a.rows || n0 + col >= a.n) return;
+  float v[8] = {}, bias[8];
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += part[i][r][col + e];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bias[e] = a.bias && n0 + col + e < a.n ? load_as(a.bias, n0 + col + e, a.bias_dtype) : 0.0f;
+  finish(a, m0 + r, n0 + col, v, bias);
 }
 
 struct LoglikesArgs {

@@ -65,6 +65,45 @@ bool rows_apart(int64_t seqs, int64_t frames, int64_t cols, int64_t seq_stride, 
   return (__int128)seq_stride >= (__int128)(frames - 1) * stride + cols || (__int128)stride >= (__int128)(seqs - 1) * seq_stride + cols;
 }
 
+// Every row starts at a multiple of 16 bytes and is a whole number of 16-byte chunks, and the 256 rows of a tile are within 2 GB.
+bool chunked(const void *p, int64_t rows, int64_t stride, int64_t k, int64_t size) {
+  return aligned(p, 16) && k * size % 16 == 0 && (rows == 1 || (stride * size % 16 == 0 && stride < ((1 << 30) - k) / size / 128));
+}
+
+template <class F> int by_type(int32_t dtype, F f) { return dtype == 0 ? f(F32{}) : dtype == 1 ? f(F16{}) : f(BF16{}); }
+
+int64_t count_tiles(const LinearArgs &a, int bm, int bn) { return ((a.rows - 1) / bm + 1) * (((int64_t)a.n - 1) / bn + 1); }
+
+template <class E, int BM, int BN, int WM, int WN, int ROW, bool DIRECT>
+int run_tiles(LinearArgs a, void *stream) {
+  a.tiles_n = (a.n - 1) / BN + 1;
+  if ((a.rows - 1) / BM + 1 > INT_MAX / a.tiles_n) return refuse("wfst_linear", "too many rows for one launch");
+  return launch("wfst_linear", linear_kernel<E, BM, BN, WM, WN, ROW, DIRECT>, count_tiles(a, BM, BN), 64 * (BM / WM) * (BN / WN), a, stream);
+}
+
+// The largest tile of which there is one for each compute unit: it reads the least per product (256 x 256: 32 bytes per clock and
+// compute unit at full rate, 128 x 128: 64, which is what a compute unit can load), but smaller ones fill the GPU earlier.
+// bf16, us, tiles of 256 x 256 / 256 x 128 / 128 x 128 / 64 x 64 (k x n): 118,417 rows, 512 x 2048: 279 / 300 / 331 / -;
+// 16,384, 2048 x 512: 49 / 44 / 47 / 57 (128, 256, 512, 2,048 tiles); 2,048, 2048 x 2048: 44 / 35 / 28 / 39 (64, 128, 256, 1,024);
+// 512, 512 x 2048: 18 / 13 / 10 / 6.  Single tiles of 16 x 16 with k shared out over the waves: 33 to 128 rows, 2048 x 512: 7.4, 64 x 64: 9.1;
+// 512 rows (1,024 tiles): 19, 64 x 64: 9.3.  In fp32 the matrix instructions bound the kernel and the larger tiles gain nothing
+// (14,803 rows, 512 x 2048: 268 / 251 / 255 / 264), nor does 256 x 256 by way of registers (511 x 2047: 482 / 476 / 531 / 931).
+template <class E> int run_linear(LinearArgs a, bool direct, void *stream) {
+  constexpr bool kHalf = sizeof(typename E::T) == 2;
+  if (count_tiles(a, 16, 16) <= 256) {
+    a.tiles_n = (a.n - 1) / 16 + 1;
+    return launch("wfst_linear", linear_few_kernel<E>, count_tiles(a, 16, 16), 512, a, stream);
+  }
+  if constexpr (kHalf) {
+    if (direct && count_tiles(a, 256, 256) >= 256) return run_tiles<E, 256, 256, 64, 64, 64, true>(a, stream);
+    if (count_tiles(a, 256, 128) >= 256)
+      return direct ? run_tiles<E, 256, 128, 64, 64, 64, true>(a, stream) : run_tiles<E, 256, 128, 64, 64, 64, false>(a, stream);
+  }
+  if (count_tiles(a, 128, 128) >= 256)
+    return direct ? run_tiles<E, 128, 128, 64, 64, 64, true>(a, stream) : run_tiles<E, 128, 128, 64, 64, 64, false>(a, stream);
+  return direct ? run_tiles<E, 64, 64, 32, 32, 128, true>(a, stream) : run_tiles<E, 64, 64, 32, 32, 128, false>(a, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -93,10 +132,9 @@ int32_t wfst_linear(const wfst_linear_args *args, void *stream) {
   if (overlap(p.y, ny, p.residual, nr) && !(p.residual == p.y && (p.residual_stride == p.y_stride || p.rows == 1)))
     return refuse(me, "y overlaps the residual without being it");
   LinearArgs a{p.x, p.w, p.bias, p.residual, p.y, p.rows, p.x_stride, p.w_stride, p.residual_stride, p.y_stride,
-               p.k, p.n, p.bias_dtype, p.out_dtype, p.activation, p.scale};
-  const int64_t tiles_m = (p.rows - 1) / 64 + 1, tiles_n = ((int64_t)p.n - 1) / 64 + 1;
-  if (tiles_m > INT_MAX / tiles_n) return refuse(me, "too many rows for one launch");
-  return launch(me, BY_TYPE(p.dtype, linear_kernel), tiles_m * tiles_n, 256, a, stream);
+               p.k, p.n, p.bias_dtype, p.out_dtype, p.activation, p.scale, 0};
+  const bool direct = chunked(p.x, p.rows, p.x_stride, p.k, size) && chunked(p.w, p.n, p.w_stride, p.k, size);
+  return by_type(p.dtype, [&](auto e) { return run_linear<decltype(e)>(a, direct, stream); });
 }
 
 int32_t wfst_loglikes(const wfst_loglikes_args *args, void *stream) {
