@@ -166,22 +166,26 @@ template <class E> __device__ __forceinline__ i32x4 chunk_of(const char *row, in
   return c;
 }
 
-// A tile of BM rows of x by BN rows of w, WM x WN of them per wave.  LDS holds kStages parts of kRow bytes of k of each row, at
+// A tile of BM rows of x by BN rows of w, WM x WN of them per wave.  LDS holds 2 or 3 parts of ROW bytes of k of each row, at
 // chunk c ^ swizzle(row): the 16 lanes that read a column of chunks together are then in different banks.
-template <class E, int BM, int BN, int WM, int WN, int ROW>
+template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES = 3>
 struct Tile {
   static constexpr int kWavesM = BM / WM, kWavesN = BN / WN, kWaves = kWavesM * kWavesN, kThreads = 64 * kWaves;
-  static constexpr int kRow = ROW, kChunks = ROW / 16;
-  static constexpr int kStage = (BM + BN) * ROW, kStages = 3;
-  static constexpr int kLoads = kStage / 1024 / kWaves;                // 1024 bytes per wave and load
+  static constexpr int kChunks = ROW / 16;
+  static constexpr int kStage = (BM + BN) * ROW, kPieces = kStage / 1024;      // 1024 bytes per wave and load
+  static constexpr int kLoads = (kPieces + kWaves - 1) / kWaves;
   static constexpr int kTM = WM / 32, kTN = WN / 32;
-  static_assert(kStage % (1024 * kWaves) == 0 && WM % 32 == 0 && WN % 32 == 0 && (ROW == 64 || ROW == 128), "whole loads per wave");
+  static_assert(kStage % 1024 == 0 && BM % (64 / kChunks) == 0 && WM % 32 == 0 && WN % 32 == 0, "whole loads, of x or of w");
+  static_assert((ROW == 64 || ROW == 128 || (ROW == 32 && STAGES == 2)) && (STAGES == 2 || STAGES == 3), "as part() takes them");
 
-  static __device__ __forceinline__ int swizzle(int row) { return ROW == 64 ? (row >> 2) & 3 : (row >> 1) & 7; }
+  static __device__ __forceinline__ int swizzle(int row) { return ROW == 32 ? (row >> 3) & 1 : ROW == 64 ? (row >> 2) & 3 : (row >> 1) & 7; }
 
   // Piece i of this wave: 1024 bytes of a stage, 64 / kChunks rows of it.  Row r of the tile is x's row r for r < BM, w's row r - BM behind
-  // that; a piece is of one of them.
-  static __device__ __forceinline__ int piece(int i) { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) + kWaves * i; }
+  // that; a piece is of one of them.  (If the waves do not share them out evenly, some load the last piece again.)
+  static __device__ __forceinline__ int piece(int i) {
+    const int n = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) + kWaves * i;
+    return kPieces % kWaves != 0 && n >= kPieces ? kPieces - 1 : n;
+  }
   static __device__ __forceinline__ int piece_row(int i) { return piece(i) * (64 / kChunks) + (threadIdx.x & 63) / kChunks; }
   static __device__ __forceinline__ int piece_chunk(int i) { return ((threadIdx.x & 63) % kChunks) ^ swizzle(piece_row(i)); }
 
@@ -241,55 +245,72 @@ struct Tile {
   }
   // One part but the last, from stage `here`: the next step's chunks are read while a step is multiplied, across the parts too.
   // Before the last step the waves meet: the part behind has arrived in `next` then, and nobody reads `here` any more, so
-  // that the part three further on can come there.
-  __device__ __forceinline__ void part(int p, Buffer x, Buffer w, char *here, char *next, Step (&f)[2], f32x16 (&acc)[kTN][kTM]) {
+  // that the part STAGES further on can come there.  F: where the part's first step is in f.
+  template <int F>
+  __device__ __forceinline__ void part(int p, Buffer x, Buffer w, char *here, char *next, Step (&f)[2], f32x16 (&acc)[kTN][kTM], bool used) {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       if (s + 1 < kSteps) {
-        read(f[(s + 1) & 1], here, s + 1);
+        read(f[(F + s + 1) & 1], here, s + 1);
       } else {
-        wait_loads<kLoads>();
+        wait_loads<(STAGES - 2) * kLoads>();
         meet();
-        read(f[0], next, 0);
+        read(f[(F + s + 1) & 1], next, 0);
         __builtin_amdgcn_sched_barrier(0);
-        load(x, w, here, p + 3);
+        load(x, w, here, p + STAGES);
       }
       __builtin_amdgcn_sched_barrier(0);             // the reads go out before the products that hide them
-      multiply(f[s & 1], acc);
+      if (used) multiply(f[(F + s) & 1], acc);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // The whole product.  Ends with all waves done with LDS.  (Three parts behind the last one are loaded too, while the last ones
-  // are multiplied, and not used: so every wait has the same number of loads behind it.)
-  __device__ __forceinline__ void product(Buffer x, Buffer w, char *s0, char *s1, char *s2, int k_bytes, f32x16 (&acc)[kTN][kTM]) {
+  // The whole product.  Ends with all waves done with LDS.  (STAGES parts behind the last one are loaded too, while the last ones
+  // are multiplied, and not used: so every wait has the same number of loads behind it.)  used: whether this wave's sums are.
+  __device__ __forceinline__ void product(Buffer x, Buffer w, char *s0, char *s1, char *s2, int k_bytes, f32x16 (&acc)[kTN][kTM], bool used = true) {
+    constexpr int kFlip = kSteps & 1;                // one step per part: the two of f take turns
     const int parts = (k_bytes + ROW - 1) / ROW;
     Step f[2];
     load(x, w, s0, 0);
     load(x, w, s1, 1);
-    load(x, w, s2, 2);
-    wait_loads<2 * kLoads>();
+    if (STAGES == 3) load(x, w, s2, 2);
+    wait_loads<(STAGES - 1) * kLoads>();
     meet();
     read(f[0], s0, 0);
     int p = 0;
-    for (; p + 3 < parts; p += 3) {
-      part(p, x, w, s0, s1, f, acc);
-      part(p + 1, x, w, s1, s2, f, acc);
-      part(p + 2, x, w, s2, s0, f, acc);
+    const char *last = s0;
+    if (STAGES == 3) {
+      for (; p + 3 < parts; p += 3) {
+        part<0>(p, x, w, s0, s1, f, acc, used);
+        part<0>(p + 1, x, w, s1, s2, f, acc, used);
+        part<0>(p + 2, x, w, s2, s0, f, acc, used);
+      }
+      if (p + 1 < parts) part<0>(p, x, w, s0, s1, f, acc, used);
+      if (p + 2 < parts) part<0>(p + 1, x, w, s1, s2, f, acc, used);
+      last = p + 1 == parts ? s0 : p + 2 == parts ? s1 : s2;
+    } else {
+      for (; p + 2 < parts; p += 2) {
+        part<0>(p, x, w, s0, s1, f, acc, used);
+        part<kFlip>(p + 1, x, w, s1, s0, f, acc, used);
+      }
+      if (p + 1 < parts) {
+        part<0>(p, x, w, s0, s1, f, acc, used);
+        if (kFlip) f[0] = f[1];
+        last = s1;
+      }
     }
-    if (p + 1 < parts) part(p, x, w, s0, s1, f, acc);
-    if (p + 2 < parts) part(p + 1, x, w, s1, s2, f, acc);
-    const char *last = p + 1 == parts ? s0 : p + 2 == parts ? s1 : s2;
+    if (used) {
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      if (s + 1 < kSteps) read(f[(s + 1) & 1], last, s + 1);
-      multiply_last(f[s & 1], s, k_bytes - (parts - 1) * ROW, acc);
+      for (int s = 0; s < kSteps; ++s) {
+        if (s + 1 < kSteps) read(f[(s + 1) & 1], last, s + 1);
+        multiply_last(f[s & 1], s, k_bytes - (parts - 1) * ROW, acc);
+      }
     }
     wait_loads<0>();
     meet();
   }
   // row_of(r): start of row r of the tile; a row behind the end may be any other one
   template <class RowOf>
-  static __device__ __forceinline__ void product_staged(RowOf row_of, char *s0, char *s1, int k_bytes, f32x16 (&acc)[kTN][kTM]) {
+  static __device__ __forceinline__ void product_staged(RowOf row_of, char *s0, char *s1, int k_bytes, f32x16 (&acc)[kTN][kTM], bool used = true) {
     const int parts = (k_bytes + ROW - 1) / ROW;
     const char *from[kLoads];
 #pragma unroll
@@ -309,7 +330,7 @@ struct Tile {
         for (int s = 0; s < kSteps; ++s) {
           Step f;
           read(f, here, s);
-          multiply(f, acc);
+          if (used) multiply(f, acc);
         }
         put(i ? s0 : s1, ahead[1 - i]);                // nobody reads there since the waves last met
         meet();
@@ -445,6 +466,8 @@ __global__ __launch_bounds__(512) void linear_few_kernel(LinearArgs a) {
   finish(a, m0 + r, n0 + col, v, bias);
 }
 
+// ---- wfst_loglikes
+
 struct LoglikesArgs {
   const void *x, *w, *bias;
   const float *log_prior;
@@ -454,38 +477,204 @@ struct LoglikesArgs {
   int32_t seqs, frames, k, v, bias_dtype, out_dtype;
 };
 
-// one workgroup of 256 per frame: a lane's class at a time, then the row's maximum and sum through LDS
-template <class E>
-__global__ __launch_bounds__(256) void loglikes_kernel(LoglikesArgs a) {
-  __shared__ float z[2048], part[256];
-  const int64_t row = blockIdx.x;
-  const int s = (int)(row / a.frames), t = (int)(row % a.frames);
-  if (a.lengths && t >= a.lengths[s]) return;
-  const typename E::T *x = static_cast<const typename E::T *>(a.x) + s * a.x_seq_stride + t * a.x_stride;
-  float m = -__builtin_inff();
-  for (int c = threadIdx.x; c < a.v; c += 256) {
-    const typename E::T *w = static_cast<const typename E::T *>(a.w) + c * a.w_stride;
-    float acc = 0.0f;
-    for (int k = 0; k < a.k; ++k) acc = __builtin_fmaf(E::get(x[k]), E::get(w[k]), acc);
-    if (a.bias) acc += load_as(a.bias, c, a.bias_dtype);
-    z[c] = acc;
-    m = fmaxf(m, acc);
+// one or two neighbouring results
+__device__ __forceinline__ void store2(void *p, int64_t i, int dtype, bool both, float v0, float v1) {
+  if (!both) { store_as(p, i, dtype, v0); return; }
+  if (dtype == 0) {
+    typedef float pair __attribute__((ext_vector_type(2), aligned(4)));
+    *reinterpret_cast<pair *>(static_cast<float *>(p) + i) = pair{v0, v1};
+  } else if (dtype == 1) {
+    typedef _Float16 pair __attribute__((ext_vector_type(2), aligned(2)));
+    *reinterpret_cast<pair *>(static_cast<_Float16 *>(p) + i) = pair{(_Float16)v0, (_Float16)v1};
+  } else {
+    typedef __bf16 pair __attribute__((ext_vector_type(2), aligned(2)));
+    *reinterpret_cast<pair *>(static_cast<__bf16 *>(p) + i) = pair{(__bf16)v0, (__bf16)v1};
   }
-  part[threadIdx.x] = m;
-  __syncthreads();
-  for (int i = 0; i < 256; ++i) m = fmaxf(m, part[i]);
-  __syncthreads();
-  float sum = 0.0f;
-  for (int c = threadIdx.x; c < a.v; c += 256) sum += exp_fast(z[c] - m);
-  part[threadIdx.x] = sum;
-  __syncthreads();
-  sum = 0.0f;
-  for (int i = 0; i < 256; ++i) sum += part[i];
-  const float ls = logf(sum);
-  for (int c = threadIdx.x; c < a.v; c += 256) {
-    float l = z[c] - m - ls;
-    if (a.log_prior) l -= a.log_prior[c];
-    store_as(a.out, s * a.out_seq_stride + t * a.out_stride + c, a.out_dtype, l);
+}
+
+// The product with log-softmax behind it: a workgroup has BM whole rows, and a wave WM x WN of the sums.  A lane has 16 sums of one row
+// per 32 classes: the row's maximum and sum are the lane's own, then its neighbour's across the half wave, then, if waves lie side
+// by side (kWavesN > 1), theirs through LDS.  The log-probabilities leave through LDS too, rows at a time and in the order of memory.
+template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES, bool DIRECT>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void loglikes_kernel(LoglikesArgs a) {
+  using T = Tile<E, BM, BN, WM, WN, ROW, STAGES>;
+  constexpr int kSize = (int)sizeof(typename E::T);
+  // Rows of results that LDS takes at a time: of each wave (two waves' in a stage), or of the workgroup (in all stages).
+  constexpr bool kAlone = T::kWavesN == 1;
+  constexpr int kRowsOut = kAlone ? (BN <= 64 ? 32 : BN <= 160 ? 16 : 8) : (T::kStage / (BN * 4) >= 16 ? 16 : 8);
+  constexpr int kLds = kAlone && 2 * kRowsOut * BN * 4 > T::kStage ? 2 * kRowsOut * BN * 4 : T::kStage;
+  static_assert(kAlone ? T::kWaves <= 4 : BM == WM && kRowsOut * BN * 4 <= T::kStage, "the results fit the stages; a wave has whole rows or a part of each");
+  __shared__ __align__(16) char s0[kLds], s1[kLds], s2[STAGES == 3 ? kLds : 16];
+  __shared__ float row_part[kAlone ? 1 : T::kWavesN][BM];
+  __shared__ __align__(16) float bias[BN], prior[BN];
+  const unsigned rows = (unsigned)a.seqs * a.frames, m0 = blockIdx.x * BM, frames = a.frames;      // (at most 2^31 - 1 rows)
+  for (int c = threadIdx.x; c < BN; c += T::kThreads) {
+    bias[c] = a.bias && c < a.v ? load_as(a.bias, c, a.bias_dtype) : 0.0f;
+    prior[c] = a.log_prior && c < a.v ? a.log_prior[c] : 0.0f;
+  }
+  // is there a frame before its sequence's length among them?
+  bool any = false;
+  for (int r = threadIdx.x; r < BM && m0 + r < rows; r += T::kThreads)
+    any |= !a.lengths || (int)((m0 + r) % frames) < a.lengths[(m0 + r) / frames];
+  if (!__syncthreads_or(any)) return;
+  const char *x = static_cast<const char *>(a.x), *w = static_cast<const char *>(a.w);
+  // Row r of x in the tile, in bytes behind x.  A frame behind the length is not read: the sequence's last one before it (or its
+  // first one) stands in.
+  auto x_offset = [&](int r) {
+    const unsigned m = m0 + r < rows ? m0 + r : rows - 1;
+    const int s = (int)(m / frames);
+    int t = (int)(m % frames);
+    if (a.lengths && t >= a.lengths[s]) t = a.lengths[s] > 0 ? a.lengths[s] - 1 : 0;
+    return (s * a.x_seq_stride + t * a.x_stride) * kSize;
+  };
+  auto w_offset = [&](int r) { return (int64_t)(r - BM < a.v ? r - BM : a.v - 1) * a.w_stride * kSize; };
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = wave / T::kWavesN, wn = wave % T::kWavesN;
+  const bool used = kAlone || wn * WN < a.v;          // waves whose classes are all behind v only load and store
+  f32x16 acc[T::kTN][T::kTM];
+#pragma unroll
+  for (int i = 0; i < T::kTN; ++i)
+#pragma unroll
+    for (int j = 0; j < T::kTM; ++j) acc[i][j] = f32x16{};
+  if (DIRECT) {
+    T t;
+    t.aim([&](int r) { return r < BM ? (int)x_offset(r) : r - BM < a.v ? (int)w_offset(r) : 0x7fffff00; });      // (out of bounds: not read)
+    const int64_t x_end = (int64_t)(a.seqs - 1) * a.x_seq_stride + (int64_t)(a.frames - 1) * a.x_stride + a.k;      // (within 2 GB here)
+    t.product(buffer(x, (uint32_t)(x_end * kSize)), buffer(w, bytes_behind(a.v, a.w_stride, a.k, kSize)), s0, s1, s2, a.k * kSize, acc, used);
+  } else {
+    T::product_staged([&](int r) { return r < BM ? x + x_offset(r) : w + w_offset(r); }, s0, s1, a.k * kSize, acc, used);
+  }
+
+  // sums -> z = sum + bias; classes behind v count as -inf
+#pragma unroll
+  for (int i = 0; i < T::kTN; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int c = wn * WN + 32 * i + 8 * q + 4 * (lane >> 5);
+      const f32x4 b = *reinterpret_cast<const f32x4 *>(bias + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < T::kTM; ++j) acc[i][j][4 * q + e] = c + e < a.v ? acc[i][j][4 * q + e] + b[e] : -__builtin_inff();
+    }
+  // the rows' maxima
+  float m[T::kTM], ls[T::kTM];
+#pragma unroll
+  for (int j = 0; j < T::kTM; ++j) {
+    m[j] = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < T::kTN; ++i)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) m[j] = fmaxf(m[j], acc[i][j][q]);
+    m[j] = fmaxf(m[j], __shfl_xor(m[j], 32));
+    if (!kAlone && lane < 32) row_part[wn][wm * WM + 32 * j + lane] = m[j];
+  }
+  if (!kAlone) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < T::kTM; ++j)
+#pragma unroll
+      for (int n = 0; n < T::kWavesN; ++n) m[j] = fmaxf(m[j], row_part[n][wm * WM + 32 * j + (lane & 31)]);
+    __syncthreads();
+  }
+  // sums of e^(z - m).  (Of -inf alone: -inf - -inf is NaN, as documented; a NaN or +inf becomes one here as well.)
+#pragma unroll
+  for (int j = 0; j < T::kTM; ++j) {
+    ls[j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < T::kTN; ++i) {
+      float part = 0.0f;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) part += exp_fast(acc[i][j][q] - m[j]);
+      ls[j] += part;
+    }
+    ls[j] += __shfl_xor(ls[j], 32);
+    if (!kAlone && lane < 32) row_part[wn][wm * WM + 32 * j + lane] = ls[j];
+  }
+  if (!kAlone) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < T::kTM; ++j) {
+      ls[j] = 0.0f;
+#pragma unroll
+      for (int n = 0; n < T::kWavesN; ++n) ls[j] += row_part[n][wm * WM + 32 * j + (lane & 31)];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < T::kTM; ++j) {
+    ls[j] = logf(ls[j]);
+#pragma unroll
+    for (int i = 0; i < T::kTN; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 off = *reinterpret_cast<const f32x4 *>(prior + wn * WN + 32 * i + 8 * q + 4 * (lane >> 5));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = ((acc[i][j][4 * q + e] - m[j]) - ls[j]) - off[e];
+      }
+  }
+
+  // rows r0.. of the results into `to`, a.v floats each: the lanes that have them write
+  auto leave = [&](float *to, int j, int r0, int n) {
+    const int r = (lane & 31) - r0;
+    if (r < 0 || r >= n) return;
+#pragma unroll
+    for (int i = 0; i < T::kTN; ++i)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        const int c = wn * WN + 32 * i + 8 * (q / 4) + 4 * (lane >> 5) + q % 4;
+        if (c < a.v) to[r * a.v + c] = acc[i][j][q];
+      }
+  };
+  if constexpr (kAlone) {
+    float *out = reinterpret_cast<float *>((wave < 2 ? s0 : s1) + (wave & 1) * (kRowsOut * BN * 4));
+#pragma unroll
+    for (int j = 0; j < T::kTM; ++j)
+      for (int r0 = 0; r0 < 32; r0 += kRowsOut) {
+        leave(out, j, r0, kRowsOut);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        const unsigned first = m0 + wm * WM + 32 * j + r0;
+        int s = (int)(first / frames), t = (int)(first % frames);
+        // a sequence's frames among them at a time: contiguous results go out as one run
+        for (int r = 0; r < kRowsOut && s < a.seqs; ++s, t = 0) {
+          const int here = kRowsOut - r < a.frames - t ? kRowsOut - r : a.frames - t;
+          const int length = a.lengths ? a.lengths[s] : a.frames;
+          const int n = length <= t ? 0 : length - t < here ? length - t : here;
+          if (n > 0 && a.out_stride == a.v) {
+            const int64_t to = s * a.out_seq_stride + t * a.out_stride;
+            for (int c = 2 * lane; c < n * a.v; c += 128)
+              store2(a.out, to + c, a.out_dtype, c + 1 < n * a.v, out[r * a.v + c], out[r * a.v + c + 1]);
+          } else {
+            for (int i = 0; i < n; ++i)
+              for (int c = 2 * lane; c < a.v; c += 128)
+                store2(a.out, s * a.out_seq_stride + (t + i) * a.out_stride + c, a.out_dtype, c + 1 < a.v, out[(r + i) * a.v + c], out[(r + i) * a.v + c + 1]);
+          }
+          r += here;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      }
+  } else {
+    // kRowsOut rows in each stage (of which two are used, so that the same code does for two and three)
+#pragma unroll
+    for (int j = 0; j < T::kTM; ++j)
+      for (int r0 = 0; r0 < 32; r0 += 2 * kRowsOut) {
+        leave(reinterpret_cast<float *>(s0), j, r0, kRowsOut);
+        leave(reinterpret_cast<float *>(s1), j, r0 + kRowsOut, kRowsOut);
+        __syncthreads();
+        for (int r = wave; r < 2 * kRowsOut; r += T::kWaves) {
+          const unsigned row = m0 + 32 * j + r0 + r;
+          if (row >= rows) break;
+          const int s = (int)(row / frames), t = (int)(row % frames);
+          if (a.lengths && t >= a.lengths[s]) continue;
+          const float *from = reinterpret_cast<const float *>(r < kRowsOut ? s0 : s1) + (r % kRowsOut) * a.v;
+          for (int c = 2 * lane; c < a.v; c += 128)
+            store2(a.out, s * a.out_seq_stride + t * a.out_stride + c, a.out_dtype, c + 1 < a.v, from[c], from[c + 1]);
+        }
+        __syncthreads();
+      }
   }
 }
 

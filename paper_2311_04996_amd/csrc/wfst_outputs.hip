@@ -104,6 +104,24 @@ template <class E> int run_linear(LinearArgs a, bool direct, void *stream) {
   return direct ? run_tiles<E, 64, 64, 32, 32, 128, true>(a, stream) : run_tiles<E, 64, 64, 32, 32, 128, false>(a, stream);
 }
 
+template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES>
+int run_rows(const LoglikesArgs &a, bool direct, void *stream) {
+  const int64_t blocks = ((int64_t)a.seqs * a.frames - 1) / BM + 1;
+  constexpr int kThreads = 64 * (BM / WM) * (BN / WN);
+  return direct ? launch("wfst_loglikes", loglikes_kernel<E, BM, BN, WM, WN, ROW, STAGES, true>, blocks, kThreads, a, stream)
+                : launch("wfst_loglikes", loglikes_kernel<E, BM, BN, WM, WN, ROW, STAGES, false>, blocks, kThreads, a, stream);
+}
+
+// The narrowest tile that has a whole row.  Up to 256 classes a wave has 32 rows of its own; behind that the waves lie side by side.
+template <class E> int run_loglikes(const LoglikesArgs &a, bool direct, void *stream) {
+  if (a.v <= 64) return run_rows<E, 128, 64, 32, 64, 64, 3>(a, direct, stream);
+  if (a.v <= 160) return run_rows<E, 128, 160, 32, 160, 64, 3>(a, direct, stream);
+  if (a.v <= 256) return run_rows<E, 128, 256, 32, 256, 64, 3>(a, direct, stream);
+  if (a.v <= 512) return run_rows<E, 64, 512, 64, 64, 64, 3>(a, direct, stream);
+  if (a.v <= 1024) return run_rows<E, 64, 1024, 64, 64, 64, 2>(a, direct, stream);
+  return run_rows<E, 32, 2048, 32, 128, 32, 2>(a, direct, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -152,6 +170,7 @@ int32_t wfst_loglikes(const wfst_loglikes_args *args, void *stream) {
   if (!aligned(p.x, size) || !aligned(p.w, size) || !aligned(p.out, out_size) || !aligned(p.log_prior, 4) || !aligned(p.lengths, 4) ||
       (p.bias && !aligned(p.bias, type_size(p.bias_dtype))))
     return refuse(me, "an address is not a multiple of its element's size");
+  if ((int64_t)p.seqs * p.frames > INT_MAX) return refuse(me, "more than 2^31 - 1 frames");
   const int64_t nx = span(p.seqs, p.frames, p.k, p.x_seq_stride, p.x_stride, size), nw = span(1, p.v, p.k, 0, p.w_stride, size);
   const int64_t no = span(p.seqs, p.frames, p.v, p.out_seq_stride, p.out_stride, out_size);
   if (nx < 0 || nw < 0 || no < 0) return refuse(me, "sizes and strides are too large");
@@ -160,7 +179,9 @@ int32_t wfst_loglikes(const wfst_loglikes_args *args, void *stream) {
     return refuse(me, "out overlaps what is read");
   LoglikesArgs a{p.x, p.w, p.bias, p.log_prior, p.lengths, p.out, p.x_seq_stride, p.x_stride, p.w_stride, p.out_seq_stride, p.out_stride,
                  p.seqs, p.frames, p.k, p.v, p.bias_dtype, p.out_dtype};
-  return launch(me, BY_TYPE(p.dtype, loglikes_kernel), (int64_t)p.seqs * p.frames, 256, a, stream);
+  const bool direct = aligned(p.x, 16) && aligned(p.w, 16) && p.k * size % 16 == 0 && p.x_seq_stride * size % 16 == 0 && p.x_stride * size % 16 == 0 &&
+                      p.w_stride * size % 16 == 0 && nx < INT_MAX - 1024 && nw < INT_MAX - 1024 && p.w_stride < (INT_MAX - 1024) / size / 2048;
+  return by_type(p.dtype, [&](auto e) { return run_loglikes<decltype(e)>(a, direct, stream); });
 }
 
 int64_t wfst_token_logprobs_workspace(int64_t, int32_t, int32_t) { return 0; }
