@@ -461,7 +461,7 @@ int32_t wfst_loglikes(const wfst_loglikes_args *args, void *stream);
  *   stats: the row's maximum and the log of sum_j e^(x[j] - maximum), whose sum lse is, for the backward call: with
  *   scores far from 0 the sum of the two no longer holds what each of them does.
  *   Any output may be NULL (logprobs too if given == 0, the top ones if top == 0).
- *   1 <= v <= 2^30, 0 <= given <= 4096, 0 <= top <= min(v, 64).
+ *   1 <= v <= 2^30, 0 <= given <= 256, 0 <= top <= min(v, 64).
  *   A row with a NaN or +inf gives NaN for lse, entropy and log-probabilities.  A row of -inf only (everything
  *   ruled out) gives lse -inf, entropy 0, log-probabilities -inf and a maximum of -inf.
  *   workspace: wfst_token_logprobs_workspace(rows, v, top) bytes (rows = seqs * frames), 16-byte aligned, used by this call alone

@@ -1,4 +1,7 @@
 // Log-probabilities of given tokens, entropy and top alternatives of rows of scores, and their gradient.
+//
+// With m a row's maximum and d = x - m: S = sum e^d, lse = m + ln S, log p = d - ln S, entropy = ln S - (sum e^d d) / S.  All four
+// come out of one reading of the row.  Every sum has a fixed order: lanes, then waves, then parts of a row.
 #ifndef WFST_LOGPROBS_H_
 #define WFST_LOGPROBS_H_
 
@@ -12,8 +15,10 @@ struct LogprobsArgs {
   float *logprobs, *lse, *entropy, *stats;
   int32_t *top_ids;
   float *top_logprobs;
+  void *workspace;
   int64_t seq_stride, stride;
   int32_t seqs, frames, v, given, top;
+  int32_t splits, split_size;                          // long rows: parts of a row, elements of a part
 };
 
 struct BackwardArgs {
@@ -25,112 +30,480 @@ struct BackwardArgs {
   void *grad_scores;
   int64_t seq_stride, stride, grad_seq_stride, grad_stride;
   int32_t seqs, frames, v, given, top;
+  int32_t splits;                                      // long rows: workgroups per row
 };
 
-// A float as a whole number that orders alike: -0 and +0 are one, every NaN is above +inf.
+constexpr int kMaxGiven = 256, kMaxTop = 64;
+constexpr int kShortRow = 2048;                        // rows of up to so many scores are held in registers
+
+// A float as a whole number that orders alike: -0 and +0 are one, every NaN is above +inf.  Never kNothing.
+constexpr int kNothing = INT32_MIN;
 __device__ __forceinline__ int order_of(float x) {
-  if (x != x) return 0x7fffffff;
-  const int b = __float_as_int(x + 0.0f);
-  return b < 0 ? b ^ 0x7fffffff : b;
+  const int b = __float_as_int(x + 0.0f), o = b < 0 ? b ^ 0x7fffffff : b;
+  return x != x ? 0x7fffffff : o;
 }
-// (order, lower index first) as one number
-__device__ __forceinline__ unsigned long long key_of(float x, int j) {
-  return ((unsigned long long)((unsigned)order_of(x) ^ 0x80000000u) << 32) | (unsigned)~j;
+__device__ __forceinline__ float float_of(int order) { return __int_as_float(order < 0 ? order ^ 0x7fffffff : order); }
+// (order, lower index first) as one number; 0 is below all of them
+__device__ __forceinline__ unsigned long long key_of(int order, int j) {
+  return ((unsigned long long)((unsigned)order ^ 0x80000000u) << 32) | (unsigned)~j;
 }
+__device__ __forceinline__ int index_of(unsigned long long key) { return (int)~(unsigned)key; }
+__device__ __forceinline__ float score_of(unsigned long long key) { return float_of((int)((unsigned)(key >> 32) ^ 0x80000000u)); }
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 
+// A row that rules everything out.  (The maximum passes over a NaN, the sum does not.)
+__device__ __forceinline__ bool is_empty(float m, float ls) { return m == neg_inf() && ls == neg_inf(); }
 // log-probability of a score in a row with this maximum and log of the sum behind it: in an empty row it is -inf
-__device__ __forceinline__ float logprob_of(float x, float m, float ls) { return m == neg_inf() ? m : (x - m) - ls; }
+__device__ __forceinline__ float logprob_of(float x, float m, float ls) { return is_empty(m, ls) ? m : (x - m) - ls; }
 
-// one workgroup of 256 per row, several passes over it
+// e^d d, 0 for d = -inf (e^d is 0 then, so that any finite d does); a NaN stays one through e^d
+__device__ __forceinline__ float weighted(float e, float d) { return e * fmaxf(d, -1e4f); }
+
+// ---- reductions over the 16 lanes of a row of the wave (rotations by 8, 4, 2, 1), or over all 64: every lane gets the result
+template <int CTRL> __device__ __forceinline__ float turned(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL> __device__ __forceinline__ int turned(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+template <int LANES, class V, class Op> __device__ __forceinline__ V reduce(V v, Op op) {
+  v = op(v, turned<0x128>(v));
+  v = op(v, turned<0x124>(v));
+  v = op(v, turned<0x122>(v));
+  v = op(v, turned<0x121>(v));
+  if (LANES == 64) {
+    v = op(v, __shfl_xor(v, 16));
+    v = op(v, __shfl_xor(v, 32));
+  }
+  return v;
+}
+template <int LANES> __device__ __forceinline__ float max_over(float v) { return reduce<LANES>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int LANES> __device__ __forceinline__ float sum_over(float v) { return reduce<LANES>(v, [](float a, float b) { return a + b; }); }
+template <int LANES> __device__ __forceinline__ int max_over(int v) { return reduce<LANES>(v, [](int a, int b) { return a > b ? a : b; }); }
+template <int LANES> __device__ __forceinline__ int min_over(int v) { return reduce<LANES>(v, [](int a, int b) { return a < b ? a : b; }); }
+
+// what a row's lse, entropy and stats are; one lane writes them
+__device__ __forceinline__ void write_row(const LogprobsArgs &a, int64_t row, float m, float sum, float weighted_sum, float ls) {
+  if (a.lse) a.lse[row] = m + ls;
+  if (a.stats) { a.stats[2 * row] = m; a.stats[2 * row + 1] = ls; }
+  if (a.entropy) a.entropy[row] = is_empty(m, ls) ? 0.0f : ls - weighted_sum / sum;
+}
 template <class E>
-__global__ __launch_bounds__(256) void logprobs_kernel(LogprobsArgs a) {
-  __shared__ float part[2][256];
-  __shared__ unsigned long long keys[256];
-  const int64_t row = blockIdx.x;
-  const int s = (int)(row / a.frames), t = (int)(row % a.frames);
-  if (a.lengths && t >= a.lengths[s]) return;
-  const typename E::T *x = static_cast<const typename E::T *>(a.scores) + s * a.seq_stride + t * a.stride;
-  const int tid = threadIdx.x;
+__device__ __forceinline__ float given_logprob(const typename E::T *x, int v, int token, float m, float ls) {
+  if (token == -1) return 0.0f;
+  if (token < 0 || token >= v) return __builtin_nanf("");
+  return logprob_of(E::get(x[token]), m, ls);
+}
+
+// ---- rows of up to 2,048 scores: LANES lanes hold a row, EACH scores per lane, in registers.  16 lanes for up to 256: a reduction
+// then stays within the rotations, and serves four rows.
+template <class E, int LANES, int EACH>
+__global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a) {
+  const int lane = threadIdx.x % LANES;
+  const unsigned row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, rows = (unsigned)a.seqs * a.frames;
+  const unsigned s = row / (unsigned)a.frames, t = row % (unsigned)a.frames;
+  // (lanes without a row go along with the others as far as they exchange values; they have no scores and write nothing)
+  const bool live = row < rows && (!a.lengths || (int)t < a.lengths[s]);
+  const typename E::T *x = static_cast<const typename E::T *>(a.scores) + (live ? s * a.seq_stride + t * a.stride : 0);
+  float z[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) z[e] = live && lane + LANES * e < a.v ? E::get(x[lane + LANES * e]) : neg_inf();
   float m = neg_inf();
-  for (int j = tid; j < a.v; j += 256) m = fmaxf(m, E::get(x[j]));
-  part[0][tid] = m;
-  __syncthreads();
-  for (int i = 0; i < 256; ++i) m = fmaxf(m, part[0][i]);
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) m = fmaxf(m, z[e]);
+  m = max_over<LANES>(m);
   const float base = m == neg_inf() ? 0.0f : m;
-  float sum = 0.0f, ent = 0.0f;
-  for (int j = tid; j < a.v; j += 256) {
-    const float d = E::get(x[j]) - base, e = exp_fast(d);
-    sum += e;
-    ent += e * fmaxf(d, -1e4f);
+  float sum = 0.0f, wsum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const float d = z[e] - base, p = exp_fast(d);
+    sum += p;
+    wsum += weighted(p, d);
   }
-  __syncthreads();
-  part[0][tid] = sum;
-  part[1][tid] = ent;
-  __syncthreads();
-  sum = ent = 0.0f;
-  for (int i = 0; i < 256; ++i) { sum += part[0][i]; ent += part[1][i]; }
-  const float ls = logf(sum), lse = m + ls;
-  if (tid == 0) {
-    if (a.lse) a.lse[row] = lse;
-    if (a.stats) { a.stats[2 * row] = m; a.stats[2 * row + 1] = ls; }
-    if (a.entropy) a.entropy[row] = m == neg_inf() && sum == 0.0f ? 0.0f : ls - ent / sum;
+  sum = sum_over<LANES>(sum);
+  wsum = sum_over<LANES>(wsum);
+  const float ls = logf(sum);
+  if (live) {
+    if (lane == 0) write_row(a, row, m, sum, wsum, ls);
+    if (a.logprobs)
+      for (int g = lane; g < a.given; g += LANES)
+        a.logprobs[(int64_t)row * a.given + g] = given_logprob<E>(x, a.v, a.tokens[(int64_t)row * a.given + g], m, ls);
   }
-  if (a.logprobs)
-    for (int g = tid; g < a.given; g += 256) {
-      const int j = a.tokens[row * a.given + g];
-      float lp = __builtin_nanf("");
-      if (j == -1) lp = 0.0f;
-      else if (j >= 0 && j < a.v) lp = logprob_of(E::get(x[j]), m, ls);
-      a.logprobs[row * a.given + g] = lp;
-    }
-  unsigned long long last = ~0ull;
+  if (a.top == 0) return;
+  // The top ones, one after the other: every lane's best, the best of them, and its lane goes on to its next one.
+  int order[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) order[e] = lane + LANES * e < a.v ? order_of(z[e]) : kNothing;
   for (int i = 0; i < a.top; ++i) {
-    unsigned long long best = 0;
-    for (int j = tid; j < a.v; j += 256) {
-      const unsigned long long k = key_of(E::get(x[j]), j);
-      if (k < last && k > best) best = k;
+    int best = order[0], at = 0;
+#pragma unroll
+    for (int e = 1; e < EACH; ++e) {                   // (of equal ones the lower index)
+      at = order[e] > best ? e : at;
+      best = order[e] > best ? order[e] : best;
     }
-    __syncthreads();
-    keys[tid] = best;
-    __syncthreads();
-    for (int q = 0; q < 256; ++q) best = keys[q] > best ? keys[q] : best;
-    last = best;
-    if (tid == 0) {
-      const int j = (int)~(unsigned)best;
-      if (a.top_ids) a.top_ids[row * a.top + i] = j;
-      if (a.top_logprobs) a.top_logprobs[row * a.top + i] = logprob_of(E::get(x[j]), m, ls);
+    const int top = max_over<LANES>(best);
+    const int j = min_over<LANES>(best == top ? lane + LANES * at : INT32_MAX);
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) order[e] = j == lane + LANES * e ? kNothing : order[e];
+    if (live && lane == 0) {
+      if (a.top_ids) a.top_ids[(int64_t)row * a.top + i] = j;
+      if (a.top_logprobs) a.top_logprobs[(int64_t)row * a.top + i] = logprob_of(float_of(top), m, ls);
     }
   }
 }
 
-// one workgroup of 256 per row; the elements that a given token or a top one names are written last
+// ---- longer rows: a workgroup per part of a row
+//
+// A lane takes 16 bytes at a time, keeps the maximum of what it has seen, and scales its sums when that grows.  The top ones need
+// no list on the way: the k-th largest of the lanes' maxima is a bound that at least k scores reach, and what reaches it
+// lies with the lanes whose own maximum does.  Those, k of 256 unless scores are equal, are read again and what reaches the bound
+// is sorted.  Rows with too many equal scores, or a NaN, have their top ones searched one after the other instead.
+constexpr int kLongThreads = 256, kLongLoads = 4, kFound = 1024;
+
+template <class E> struct Chunk {                       // 16 bytes of scores, from any address
+  static constexpr int kN = 16 / (int)sizeof(typename E::T);
+  typedef typename E::T Vec __attribute__((ext_vector_type(16 / sizeof(typename E::T))));
+  typedef Vec Any __attribute__((aligned(sizeof(typename E::T))));
+  static __device__ __forceinline__ Vec load(const typename E::T *p) { return *reinterpret_cast<const Any *>(p); }
+  static __device__ __forceinline__ void store(typename E::T *p, Vec v) { *reinterpret_cast<Any *>(p) = v; }
+};
+
+struct Sums { float m, sum, wsum; };                    // maximum, sum of e^(x - m), sum of e^(x - m) (x - m)
+
+// the sums of two parts as one; a part without scores has m = -inf and sums of 0
+__device__ __forceinline__ Sums join(Sums p, Sums q) {
+  const float m = fmaxf(p.m, q.m), base = m == neg_inf() ? 0.0f : m;
+  const float dp = p.m - base, dq = q.m - base, ep = exp_fast(dp), eq = exp_fast(dq);
+  Sums r;
+  r.m = m;
+  r.sum = ep * p.sum + eq * q.sum;
+  r.wsum = ep * (p.wsum + fmaxf(dp, -1e4f) * p.sum) + eq * (q.wsum + fmaxf(dq, -1e4f) * q.sum);
+  return r;
+}
+
+template <class E> __device__ __forceinline__ float chunk_max(typename Chunk<E>::Vec c) {
+  float m = E::get(c[0]);
+#pragma unroll
+  for (int i = 1; i < Chunk<E>::kN; ++i) m = fmaxf(m, E::get(c[i]));
+  return m;
+}
+template <class E> __device__ __forceinline__ void add_chunk(Sums &s, typename Chunk<E>::Vec c, float base) {
+#pragma unroll
+  for (int i = 0; i < Chunk<E>::kN; ++i) {
+    const float d = E::get(c[i]) - base, e = exp_fast(d);
+    s.sum += e;
+    s.wsum += weighted(e, d);
+  }
+}
+// the maximum grows to m
+__device__ __forceinline__ float grow(Sums &s, float m) {
+  const float base = m == neg_inf() ? 0.0f : m, d = s.m - base, e = exp_fast(d);
+  s.wsum = e * (s.wsum + fmaxf(d, -1e4f) * s.sum);
+  s.sum *= e;
+  s.m = m;
+  return base;
+}
+
+// A part of a row as it is left for the kernel that joins them: sums, then `top` keys, falling.
+struct Part { Sums s; float pad; };
+__device__ __forceinline__ int64_t part_bytes(int top) { return 16 + 8 * (int64_t)top; }
+
+// What is left of a row once its sums are known, by all threads of a workgroup.  keys: its top ones, falling.
 template <class E>
-__global__ __launch_bounds__(256) void logprobs_backward_kernel(BackwardArgs a) {
-  const int64_t row = blockIdx.x;
-  const int s = (int)(row / a.frames), t = (int)(row % a.frames);
-  if (a.lengths && t >= a.lengths[s]) return;
+__device__ __forceinline__ void finish_row(const LogprobsArgs &a, int64_t row, const typename E::T *x, Sums s, const unsigned long long *keys) {
+  const float ls = logf(s.sum);
+  if (threadIdx.x == 0) write_row(a, row, s.m, s.sum, s.wsum, ls);
+  if (a.logprobs)
+    for (int g = threadIdx.x; g < a.given; g += blockDim.x)
+      a.logprobs[row * a.given + g] = given_logprob<E>(x, a.v, a.tokens[row * a.given + g], s.m, ls);
+  for (int i = threadIdx.x; i < a.top; i += blockDim.x) {
+    if (a.top_ids) a.top_ids[row * a.top + i] = index_of(keys[i]);
+    if (a.top_logprobs) a.top_logprobs[row * a.top + i] = logprob_of(score_of(keys[i]), s.m, ls);
+  }
+}
+
+template <class E>
+__global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArgs a) {
+  using C = Chunk<E>;
+  constexpr int kWaves = kLongThreads / 64, kStep = kLongThreads * C::kN;       // elements that the workgroup loads at a time
+  __shared__ Sums waves[kWaves];
+  __shared__ __align__(16) int lane_max[kLongThreads];
+  __shared__ int picked[kMaxTop], n_picked, n_found;
+  __shared__ unsigned long long found[kFound], keys[kMaxTop], best[kWaves];
+  const unsigned row = blockIdx.x / (unsigned)a.splits, split = blockIdx.x % (unsigned)a.splits;
+  const unsigned s = row / (unsigned)a.frames, t = row % (unsigned)a.frames;
+  if (a.lengths && (int)t >= a.lengths[s]) return;
+  const typename E::T *x = static_cast<const typename E::T *>(a.scores) + s * a.seq_stride + t * a.stride;
+  const int lo = split * a.split_size, hi = a.v - lo < a.split_size ? a.v : lo + a.split_size;
+  const int tid = threadIdx.x, mine = lo + tid * C::kN;        // this lane's first chunk; the next ones are kStep apart
+  Sums q = {neg_inf(), 0.0f, 0.0f};
+  int64_t j = mine;
+  for (; lo + (j - mine) + (int64_t)kStep * kLongLoads <= hi; j += kStep * kLongLoads) {
+    typename C::Vec c[kLongLoads];
+#pragma unroll
+    for (int i = 0; i < kLongLoads; ++i) c[i] = C::load(x + j + i * kStep);
+    float m = q.m;
+#pragma unroll
+    for (int i = 0; i < kLongLoads; ++i) m = fmaxf(m, chunk_max<E>(c[i]));
+    const float base = grow(q, m);
+#pragma unroll
+    for (int i = 0; i < kLongLoads; ++i) add_chunk<E>(q, c[i], base);
+  }
+  for (; j < hi; j += kStep) {                                  // the rest, whose last chunk may be cut
+    typename C::Vec c;
+    if (j + C::kN <= hi) {
+      c = C::load(x + j);
+    } else {
+#pragma unroll
+      for (int i = 0; i < C::kN; ++i) c[i] = j + i < hi ? x[j + i] : (typename E::T)neg_inf();
+    }
+    const float base = grow(q, fmaxf(q.m, chunk_max<E>(c)));
+    add_chunk<E>(q, c, base);
+  }
+  if (a.top) lane_max[tid] = mine < hi ? order_of(q.m) : kNothing;
+  if (tid == 0) n_picked = n_found = 0;
+
+  // the workgroup's sums: lanes, then waves
+  const float m = max_over<64>(q.m);
+  grow(q, m);
+  q.sum = sum_over<64>(q.sum);
+  q.wsum = sum_over<64>(q.wsum);
+  if (tid % 64 == 0) waves[tid / 64] = q;
+  __syncthreads();
+  q = waves[0];
+#pragma unroll
+  for (int i = 1; i < kWaves; ++i) q = join(q, waves[i]);
+
+  if (a.top) {
+    bool slow = q.sum != q.sum;                                 // a NaN (or +inf): maxima pass over it
+    const int n = a.top < hi - lo ? a.top : hi - lo;            // (a row's last part may be shorter)
+    if (!slow) {
+      // the bound: the n-th largest of the lanes' maxima (the lane breaks ties)
+      const int own = lane_max[tid];
+      int rank = 0;
+      for (int i = 0; i < kLongThreads; i += 4) {
+        const int4 o = *reinterpret_cast<const int4 *>(lane_max + i);
+        rank += (o.x > own || (o.x == own && i < tid)) + (o.y > own || (o.y == own && i + 1 < tid)) +
+                (o.z > own || (o.z == own && i + 2 < tid)) + (o.w > own || (o.w == own && i + 3 < tid));
+      }
+      if (rank == n - 1) picked[0] = own;
+      __syncthreads();
+      const int bound = picked[0];
+      __syncthreads();
+      if (own >= bound && own != kNothing) {
+        const int i = atomicAdd(&n_picked, 1);
+        if (i < kMaxTop) picked[i] = tid;
+      }
+      __syncthreads();
+      slow = n_picked > kMaxTop;
+      if (!slow) {
+        // the picked lanes' chunks again, all threads
+        const int chunks = (hi - lo - 1) / kStep + 1;           // of a lane, at most
+        for (int64_t i = tid; i < (int64_t)n_picked * chunks; i += kLongThreads) {
+          const int64_t at = lo + picked[i / chunks] * C::kN + (i % chunks) * kStep;
+          for (int e = 0; e < C::kN && at + e < hi; ++e) {
+            const int o = order_of(E::get(x[at + e]));
+            if (o >= bound) {
+              const int f = atomicAdd(&n_found, 1);
+              if (f < kFound) found[f] = key_of(o, (int)(at + e));
+            }
+          }
+        }
+        __syncthreads();
+        slow = n_found > kFound;
+        if (!slow) {
+          // every key's place among them, whatever order they came in
+          for (int i = tid; i < n_found; i += kLongThreads) {
+            const unsigned long long k = found[i];
+            int place = 0;
+            for (int f = 0; f < n_found; ++f) place += found[f] > k;
+            if (place < n) keys[place] = k;
+          }
+        }
+      }
+    }
+    if (slow) {                                                 // one after the other
+      unsigned long long last = ~0ull;
+      for (int i = 0; i < n; ++i) {
+        unsigned long long k = 0;
+        for (int64_t e = lo + tid; e < hi; e += kLongThreads) {
+          const unsigned long long c = key_of(order_of(E::get(x[e])), (int)e);
+          k = c < last && c > k ? c : k;
+        }
+        for (int d = 1; d < 64; d <<= 1) {
+          const unsigned long long o = __shfl_xor(k, d);
+          k = o > k ? o : k;
+        }
+        __syncthreads();
+        if (tid % 64 == 0) best[tid / 64] = k;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) k = best[w] > k ? best[w] : k;
+        last = k;
+        if (tid == 0) keys[i] = k;
+      }
+    }
+    for (int i = n + tid; i < a.top; i += kLongThreads) keys[i] = 0;
+    __syncthreads();
+  }
+  if (a.splits == 1) {
+    finish_row<E>(a, row, x, q, keys);
+  } else {
+    char *to = static_cast<char *>(a.workspace) + ((int64_t)row * a.splits + split) * part_bytes(a.top);
+    if (tid == 0) *reinterpret_cast<Part *>(to) = Part{q, 0.0f};
+    for (int i = tid; i < a.top; i += kLongThreads) reinterpret_cast<unsigned long long *>(to + 16)[i] = keys[i];
+  }
+}
+
+// The parts of a row (at most 64) as one, a wave per row: sums in the order of the parts, and the best of the parts' next keys, `top` times.
+template <class E>
+__global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsArgs a) {
+  __shared__ unsigned long long keys[kMaxTop];
+  const unsigned row = blockIdx.x, s = row / (unsigned)a.frames, t = row % (unsigned)a.frames;
+  if (a.lengths && (int)t >= a.lengths[s]) return;
+  const typename E::T *x = static_cast<const typename E::T *>(a.scores) + s * a.seq_stride + t * a.stride;
+  const char *from = static_cast<const char *>(a.workspace) + (int64_t)row * a.splits * part_bytes(a.top);
+  Sums q = {neg_inf(), 0.0f, 0.0f};
+  const int lane = threadIdx.x;
+  if (lane < a.splits) q = reinterpret_cast<const Part *>(from + lane * part_bytes(a.top))->s;
+  const float m = max_over<64>(q.m);
+  grow(q, m);
+  q.sum = sum_over<64>(q.sum);
+  q.wsum = sum_over<64>(q.wsum);
+  const unsigned long long *mine = reinterpret_cast<const unsigned long long *>(from + lane * part_bytes(a.top) + 16);
+  int next = 0;
+  unsigned long long head = lane < a.splits && a.top ? mine[0] : 0;
+  for (int i = 0; i < a.top; ++i) {
+    unsigned long long k = head;
+    for (int d = 1; d < 64; d <<= 1) {
+      const unsigned long long o = __shfl_xor(k, d);
+      k = o > k ? o : k;
+    }
+    if (lane == 0) keys[i] = k;
+    if (head == k && k) head = ++next < a.top ? mine[next] : 0;
+  }
+  __syncthreads();
+  finish_row<E>(a, row, x, q, keys);
+}
+
+// ---- the gradient
+struct Slope { float c, gh, h, m, ls; };                // of a row: p (c - gh (log p + h))
+__device__ __forceinline__ float grad_of(float x, Slope r) {
+  const float lp = (x - r.m) - r.ls;
+  return exp_fast(lp) * (r.c - r.gh * (fmaxf(lp, -1e4f) + r.h));
+}
+// Token i of the given and the top ones, and its gradient; -1 if it has none.
+__device__ __forceinline__ int named(const BackwardArgs &a, int64_t row, int i, float &g) {
+  if (i < a.given) {
+    g = a.grad_logprobs[row * a.given + i];
+    const int j = a.tokens[row * a.given + i];
+    return j >= 0 && j < a.v ? j : -1;
+  }
+  g = a.grad_top[row * a.top + (i - a.given)];
+  return a.top_ids[row * a.top + (i - a.given)];
+}
+
+template <class E, int LANES, int EACH>
+__global__ __launch_bounds__(256) void backward_short_kernel(BackwardArgs a) {
+  const int lane = threadIdx.x % LANES;
+  const unsigned row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, rows = (unsigned)a.seqs * a.frames;
+  const unsigned s = row / (unsigned)a.frames, t = row % (unsigned)a.frames;
+  if (row >= rows || (a.lengths && (int)t >= a.lengths[s])) return;      // (nothing is exchanged between lanes)
   const typename E::T *x = static_cast<const typename E::T *>(a.scores) + s * a.seq_stride + t * a.stride;
   typename E::T *dx = static_cast<typename E::T *>(a.grad_scores) + s * a.grad_seq_stride + t * a.grad_stride;
-  const float m = a.stats[2 * row], ls = a.stats[2 * row + 1], h = a.grad_entropy ? a.entropy[row] : 0.0f, gh = a.grad_entropy ? a.grad_entropy[row] : 0.0f;
-  const bool empty = m == neg_inf();
-  float c = a.grad_lse ? a.grad_lse[row] : 0.0f;
-  for (int g = 0; a.grad_logprobs && g < a.given; ++g) {
-    const int j = a.tokens[row * a.given + g];
-    if (j >= 0 && j < a.v) c -= a.grad_logprobs[row * a.given + g];
+  float z[EACH], extra[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    z[e] = lane + LANES * e < a.v ? E::get(x[lane + LANES * e]) : neg_inf();
+    extra[e] = 0.0f;
   }
-  for (int i = 0; a.grad_top && i < a.top; ++i) c -= a.grad_top[row * a.top + i];
-  for (int j = threadIdx.x; j < a.v; j += 256) {
+  Slope r;
+  r.m = a.stats[2 * (int64_t)row];
+  r.ls = a.stats[2 * (int64_t)row + 1];
+  r.c = a.grad_lse ? a.grad_lse[row] : 0.0f;
+  r.gh = a.grad_entropy ? a.grad_entropy[row] : 0.0f;
+  r.h = a.grad_entropy ? a.entropy[row] : 0.0f;
+  for (int i = 0; i < a.given + a.top; ++i) {          // every lane of the row goes over all of them, in their order
+    float g;
+    const int j = named(a, row, i, g);
+    if (j < 0) continue;
+    r.c -= g;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) extra[e] += j == lane + LANES * e ? g : 0.0f;
+  }
+  const bool empty = is_empty(r.m, r.ls);
+#pragma unroll
+  for (int e = 0; e < EACH; ++e)
+    if (lane + LANES * e < a.v) dx[lane + LANES * e] = E::put(empty ? 0.0f : grad_of(z[e], r) + extra[e]);
+}
+
+// A workgroup per part of a long row.  Scores that a token names are read first (the gradient may take the scores' place) and
+// written last, after the rest of the part.
+template <class E>
+__global__ __launch_bounds__(kLongThreads) void backward_long_kernel(BackwardArgs a) {
+  using C = Chunk<E>;
+  constexpr int kStep = kLongThreads * C::kN, kPart = kStep * kLongLoads;
+  constexpr int kNamed = kMaxGiven + kMaxTop, kMine = (kNamed + kLongThreads - 1) / kLongThreads;
+  __shared__ int ids[kNamed];
+  __shared__ float grads[kNamed];
+  const unsigned row = blockIdx.x / (unsigned)a.splits, split = blockIdx.x % (unsigned)a.splits;
+  const unsigned s = row / (unsigned)a.frames, t = row % (unsigned)a.frames;
+  if (a.lengths && (int)t >= a.lengths[s]) return;
+  const typename E::T *x = static_cast<const typename E::T *>(a.scores) + s * a.seq_stride + t * a.stride;
+  typename E::T *dx = static_cast<typename E::T *>(a.grad_scores) + s * a.grad_seq_stride + t * a.grad_stride;
+  const int64_t lo = (int64_t)split * kPart, hi = a.v - lo < kPart ? a.v : lo + kPart;
+  const int tid = threadIdx.x, n = a.given + a.top;
+  typename C::Vec c[kLongLoads];
+#pragma unroll
+  for (int i = 0; i < kLongLoads; ++i) {
+    const int64_t j = lo + tid * C::kN + i * kStep;
+    if (j + C::kN <= hi) {
+      c[i] = C::load(x + j);
+    } else {
+#pragma unroll
+      for (int e = 0; e < C::kN; ++e) c[i][e] = j + e < hi ? x[j + e] : (typename E::T)0.0f;
+    }
+  }
+  for (int i = tid; i < n; i += kLongThreads) ids[i] = named(a, row, i, grads[i]);
+  Slope r;
+  r.m = a.stats[2 * (int64_t)row];
+  r.ls = a.stats[2 * (int64_t)row + 1];
+  r.c = a.grad_lse ? a.grad_lse[row] : 0.0f;
+  r.gh = a.grad_entropy ? a.grad_entropy[row] : 0.0f;
+  r.h = a.grad_entropy ? a.entropy[row] : 0.0f;
+  const bool empty = is_empty(r.m, r.ls);
+  __syncthreads();
+  for (int i = 0; i < n; ++i) r.c -= ids[i] >= 0 ? grads[i] : 0.0f;
+  float late[kMine];
+  int where[kMine];
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int i = tid + k * kLongThreads, j = i < n ? ids[i] : -1;
+    where[k] = j >= lo && j < hi ? j : -1;
+    for (int f = 0; f < i && where[k] >= 0; ++f)
+      if (ids[f] == j) where[k] = -1;                  // the first that names it does it
+    if (where[k] < 0) continue;
     float extra = 0.0f;
-    for (int g = 0; a.grad_logprobs && g < a.given; ++g)
-      if (a.tokens[row * a.given + g] == j) extra += a.grad_logprobs[row * a.given + g];
-    for (int i = 0; a.grad_top && i < a.top; ++i)
-      if (a.top_ids[row * a.top + i] == j) extra += a.grad_top[row * a.top + i];
-    const float lp = (E::get(x[j]) - m) - ls, p = exp_fast(lp);
-    float v = p * (c - gh * (fmaxf(lp, -1e4f) + h)) + extra;
-    dx[j] = E::put(empty ? 0.0f : v);
+    for (int f = i; f < n; ++f) extra += ids[f] == j ? grads[f] : 0.0f;
+    late[k] = empty ? 0.0f : grad_of(E::get(x[j]), r) + extra;
   }
+  __syncthreads();                                     // the named scores have been read
+#pragma unroll
+  for (int i = 0; i < kLongLoads; ++i) {
+    const int64_t j = lo + tid * C::kN + i * kStep;
+    typename C::Vec d;
+#pragma unroll
+    for (int e = 0; e < C::kN; ++e) d[e] = E::put(empty ? 0.0f : grad_of(E::get(c[i][e]), r));
+    if (j + C::kN <= hi) {
+      C::store(dx + j, d);
+    } else {
+#pragma unroll
+      for (int e = 0; e < C::kN; ++e)
+        if (j + e < hi) dx[j + e] = d[e];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kMine; ++k)
+    if (where[k] >= 0) dx[where[k]] = E::put(late[k]);
 }
 
 }  // namespace wfst_ops

@@ -36,9 +36,6 @@ int launch(const char *what, void (*kernel)(Args), int64_t workgroups, int threa
   return wfst_note_error(WFST_ERR_HIP, msg);
 }
 
-// kernel<element type> of a template by the run-time type
-#define BY_TYPE(dtype, kernel) ((dtype) == 0 ? kernel<F32> : (dtype) == 1 ? kernel<F16> : kernel<BF16>)
-
 bool type_ok(int32_t t) { return t >= 0 && t <= 2; }
 int64_t type_size(int32_t t) { return t == 0 ? 4 : 2; }
 bool aligned(const void *p, int64_t to) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)to == 0; }
@@ -122,6 +119,43 @@ template <class E> int run_loglikes(const LoglikesArgs &a, bool direct, void *st
   return run_rows<E, 32, 2048, 32, 128, 32, 2>(a, direct, stream);
 }
 
+// Long rows are cut until there are about 1,024 workgroups, into parts of 8,192 scores at least and 64 of them at most.
+int row_splits(int64_t rows, int32_t v) {
+  if (v <= kShortRow) return 1;
+  const int64_t most = (v - 1) / 8192 + 1, want = (1024 - 1) / rows + 1;
+  const int64_t n = want < most ? want : most;
+  return (int)(n < 64 ? n : 64);
+}
+
+template <class E> int run_logprobs(LogprobsArgs a, void *stream) {
+  const char *me = "wfst_token_logprobs";
+  const int64_t rows = (int64_t)a.seqs * a.frames;
+  if (a.v <= 64) return launch(me, logprobs_short_kernel<E, 16, 4>, (rows - 1) / 16 + 1, 256, a, stream);
+  if (a.v <= 160) return launch(me, logprobs_short_kernel<E, 16, 10>, (rows - 1) / 16 + 1, 256, a, stream);
+  if (a.v <= 256) return launch(me, logprobs_short_kernel<E, 16, 16>, (rows - 1) / 16 + 1, 256, a, stream);
+  if (a.v <= 512) return launch(me, logprobs_short_kernel<E, 64, 8>, (rows - 1) / 4 + 1, 256, a, stream);
+  if (a.v <= 1024) return launch(me, logprobs_short_kernel<E, 64, 16>, (rows - 1) / 4 + 1, 256, a, stream);
+  if (a.v <= kShortRow) return launch(me, logprobs_short_kernel<E, 64, 32>, (rows - 1) / 4 + 1, 256, a, stream);
+  a.splits = row_splits(rows, a.v);
+  a.split_size = ((a.v - 1) / a.splits / 8 + 1) * 8;
+  const int rc = launch(me, logprobs_long_kernel<E>, rows * a.splits, kLongThreads, a, stream);
+  return rc != WFST_OK || a.splits == 1 ? rc : launch(me, logprobs_join_kernel<E>, rows, 64, a, stream);
+}
+
+template <class E> int run_backward(BackwardArgs a, void *stream) {
+  const char *me = "wfst_token_logprobs_backward";
+  const int64_t rows = (int64_t)a.seqs * a.frames;
+  if (a.v <= 64) return launch(me, backward_short_kernel<E, 16, 4>, (rows - 1) / 16 + 1, 256, a, stream);
+  if (a.v <= 160) return launch(me, backward_short_kernel<E, 16, 10>, (rows - 1) / 16 + 1, 256, a, stream);
+  if (a.v <= 256) return launch(me, backward_short_kernel<E, 16, 16>, (rows - 1) / 16 + 1, 256, a, stream);
+  if (a.v <= 512) return launch(me, backward_short_kernel<E, 64, 8>, (rows - 1) / 4 + 1, 256, a, stream);
+  if (a.v <= 1024) return launch(me, backward_short_kernel<E, 64, 16>, (rows - 1) / 4 + 1, 256, a, stream);
+  if (a.v <= kShortRow) return launch(me, backward_short_kernel<E, 64, 32>, (rows - 1) / 4 + 1, 256, a, stream);
+  const int part = kLongThreads * kLongLoads * Chunk<E>::kN;
+  a.splits = (a.v - 1) / part + 1;
+  return launch(me, backward_long_kernel<E>, rows * a.splits, kLongThreads, a, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -184,7 +218,11 @@ int32_t wfst_loglikes(const wfst_loglikes_args *args, void *stream) {
   return by_type(p.dtype, [&](auto e) { return run_loglikes<decltype(e)>(a, direct, stream); });
 }
 
-int64_t wfst_token_logprobs_workspace(int64_t, int32_t, int32_t) { return 0; }
+int64_t wfst_token_logprobs_workspace(int64_t rows, int32_t v, int32_t top) {
+  if (rows < 1 || v < 1 || top < 0) return 0;
+  const int splits = row_splits(rows, v);
+  return splits == 1 ? 0 : rows * splits * (16 + 8 * (int64_t)top);
+}
 
 int32_t wfst_token_logprobs(const wfst_token_logprobs_args *args, void *stream) {
   const char *me = "wfst_token_logprobs";
@@ -193,8 +231,8 @@ int32_t wfst_token_logprobs(const wfst_token_logprobs_args *args, void *stream) 
   if (!type_ok(p.dtype)) return refuse(me, "unknown element type");
   if (p.seqs < 0 || p.frames < 0) return refuse(me, "seqs and frames must be >= 0");
   if (p.v < 1 || p.v > (1 << 30)) return refuse(me, "v must be 1 to 2^30");
-  if (p.given < 0 || p.given > 4096) return refuse(me, "given must be 0 to 4096");
-  if (p.top < 0 || p.top > 64 || p.top > p.v) return refuse(me, "top must be 0 to 64, and at most v");
+  if (p.given < 0 || p.given > kMaxGiven) return refuse(me, "given must be 0 to 256");
+  if (p.top < 0 || p.top > kMaxTop || p.top > p.v) return refuse(me, "top must be 0 to 64, and at most v");
   if (p.seqs == 0 || p.frames == 0) return WFST_OK;
   if (!p.scores || (p.given && p.logprobs && !p.tokens)) return refuse(me, "null scores or tokens");
   if (p.seq_stride < 0 || p.stride < 0) return refuse(me, "negative stride");
@@ -220,9 +258,9 @@ int32_t wfst_token_logprobs(const wfst_token_logprobs_args *args, void *stream) 
       if (overlap(wrote[i].p, wrote[i].n, wrote[j].p, wrote[j].n)) return refuse(me, "two outputs overlap");
   }
   LogprobsArgs a{p.scores, p.tokens, p.lengths, p.given ? p.logprobs : nullptr, p.lse, p.entropy, p.stats, p.top ? p.top_ids : nullptr,
-                 p.top ? p.top_logprobs : nullptr, p.seq_stride, p.stride, p.seqs, p.frames, p.v, p.given, p.top};
+                 p.top ? p.top_logprobs : nullptr, p.workspace, p.seq_stride, p.stride, p.seqs, p.frames, p.v, p.given, p.top, 1, 0};
   if (!a.top_ids && !a.top_logprobs) a.top = 0;
-  return launch(me, BY_TYPE(p.dtype, logprobs_kernel), rows, 256, a, stream);
+  return by_type(p.dtype, [&](auto e) { return run_logprobs<decltype(e)>(a, stream); });
 }
 
 int32_t wfst_token_logprobs_backward(const wfst_token_logprobs_backward_args *args, void *stream) {
@@ -232,8 +270,8 @@ int32_t wfst_token_logprobs_backward(const wfst_token_logprobs_backward_args *ar
   if (!type_ok(p.dtype)) return refuse(me, "unknown element type");
   if (p.seqs < 0 || p.frames < 0) return refuse(me, "seqs and frames must be >= 0");
   if (p.v < 1 || p.v > (1 << 30)) return refuse(me, "v must be 1 to 2^30");
-  if (p.given < 0 || p.given > 4096) return refuse(me, "given must be 0 to 4096");
-  if (p.top < 0 || p.top > 64 || p.top > p.v) return refuse(me, "top must be 0 to 64, and at most v");
+  if (p.given < 0 || p.given > kMaxGiven) return refuse(me, "given must be 0 to 256");
+  if (p.top < 0 || p.top > kMaxTop || p.top > p.v) return refuse(me, "top must be 0 to 64, and at most v");
   if (p.seqs == 0 || p.frames == 0) return WFST_OK;
   if (!p.scores || !p.stats || !p.grad_scores) return refuse(me, "null scores, stats or grad_scores");
   if (p.given && p.grad_logprobs && !p.tokens) return refuse(me, "grad_logprobs without tokens");
@@ -259,10 +297,10 @@ int32_t wfst_token_logprobs_backward(const wfst_token_logprobs_backward_args *ar
       overlap(p.grad_scores, ng, p.grad_top, rows * p.top * 4))
     return refuse(me, "grad_scores overlaps what is read");
   BackwardArgs a{p.scores, p.tokens, p.lengths, p.stats, p.entropy, p.top_ids, p.grad_logprobs, p.grad_lse, p.grad_entropy, p.grad_top,
-                 p.grad_scores, p.seq_stride, p.stride, p.grad_seq_stride, p.grad_stride, p.seqs, p.frames, p.v, p.given, p.top};
+                 p.grad_scores, p.seq_stride, p.stride, p.grad_seq_stride, p.grad_stride, p.seqs, p.frames, p.v, p.given, p.top, 1};
   if (!a.grad_logprobs) a.given = 0;
   if (!a.grad_top) a.top = 0;
-  return launch(me, BY_TYPE(p.dtype, logprobs_backward_kernel), rows, 256, a, stream);
+  return by_type(p.dtype, [&](auto e) { return run_backward<decltype(e)>(a, stream); });
 }
 
 }  // extern "C"

@@ -79,7 +79,7 @@ def tlp(**kw):
 
 @pytest.mark.parametrize("kw, word", [
     (dict(dtype=3), "type"), (dict(seqs=-1), "seqs"), (dict(frames=-1), "seqs"), (dict(v=0), "2^30"), (dict(v=(1 << 30) + 1), "2^30"),
-    (dict(given=-1), "4096"), (dict(given=4097), "4096"), (dict(top=-1), "64"), (dict(top=65), "64"), (dict(top=5, v=4), "at most v"),
+    (dict(given=-1), "256"), (dict(given=257), "256"), (dict(top=-1), "64"), (dict(top=65), "64"), (dict(top=5, v=4), "at most v"),
     (dict(scores=None), "null"), (dict(tokens=None), "null"), (dict(stride=-1), "stride"), (dict(seq_stride=-1), "stride"),
     (dict(scores=A + 1), "multiple"), (dict(tokens=2 * A + 2), "multiple"), (dict(lse=5 * A + 2), "multiple"), (dict(top_ids=7 * A + 1), "multiple"),
     (dict(seq_stride=1 << 62), "large"), (dict(seqs=1 << 17, frames=1 << 17), "rows"),
@@ -113,7 +113,7 @@ def bwd(**kw):
 
 
 @pytest.mark.parametrize("kw, word", [
-    (dict(dtype=3), "type"), (dict(seqs=-1), "seqs"), (dict(v=0), "2^30"), (dict(given=4097), "4096"), (dict(top=65), "64"),
+    (dict(dtype=3), "type"), (dict(seqs=-1), "seqs"), (dict(v=0), "2^30"), (dict(given=257), "256"), (dict(top=65), "64"),
     (dict(scores=None), "null"), (dict(stats=None), "null"), (dict(grad_scores=None), "null"), (dict(tokens=None), "without tokens"),
     (dict(entropy=None), "without entropy"), (dict(top_ids=None), "without top_ids"), (dict(stride=-1), "stride"),
     (dict(grad_stride=28), "rows of grad_scores"), (dict(grad_seq_stride=100), "rows of grad_scores"), (dict(grad_scores=11 * A + 2), "multiple"),
