@@ -458,8 +458,8 @@ int32_t wfst_loglikes(const wfst_loglikes_args *args, void *stream);
  *   contiguous over rows (s, t).  lengths as in wfst_loglikes: rows t >= lengths[s] are neither read nor written.
  *   tokens: int32, -1 = none (log-probability 0); any other value outside [0, v) gives NaN.
  *   top_ids: by falling score, equal scores by the lower index; a NaN counts as larger than every number.
- *   stats: the row's maximum and the log of sum_j e^(x[j] - maximum), whose sum lse is, for the backward call: with
- *   scores far from 0 the sum of the two no longer holds what each of them does.
+ *   maximum, log_sum: the row's maximum and the log of sum_j e^(x[j] - maximum), whose sum lse is, for the backward
+ *   call: with scores far from 0 the sum of the two no longer holds what each of them does.
  *   Any output may be NULL (logprobs too if given == 0, the top ones if top == 0).
  *   1 <= v <= 2^30, 0 <= given <= 256, 0 <= top <= min(v, 64).
  *   A row with a NaN or +inf gives NaN for lse, entropy and log-probabilities.  A row of -inf only (everything
@@ -474,7 +474,8 @@ typedef struct {
   float *logprobs;                /* [seqs][frames][given] */
   float *lse;                     /* [seqs][frames] */
   float *entropy;                 /* [seqs][frames] */
-  float *stats;                   /* [seqs][frames][2] */
+  float *maximum;                 /* [seqs][frames] */
+  float *log_sum;                 /* [seqs][frames] */
   int32_t *top_ids;               /* [seqs][frames][top] */
   float *top_logprobs;            /* [seqs][frames][top] */
   void *workspace;
@@ -493,7 +494,7 @@ int32_t wfst_token_logprobs(const wfst_token_logprobs_args *args, void *stream);
  *                    + the grad_logprobs of the tokens that are j + the grad_top of the top ones that are j
  * (the indices of the top ones are constants).  A token outside [0, v) has no gradient; a token given several times
  * has the sum of its gradients; a row of -inf only has the gradient 0; a -inf among finite scores takes the formula's value
- * with p[j] = 0.  stats (always) and entropy (if grad_entropy is given) are the forward call's.  Gradients that are
+ * with p[j] = 0.  maximum and log_sum (always) and entropy (if grad_entropy is given) are the forward call's.  Gradients that are
  * NULL count as 0.  grad_scores has the scores' type and may be the scores themselves (same address and strides), and must
  * not overlap anything else.  Frames t >= lengths[s] are neither read nor written.
  */
@@ -501,7 +502,8 @@ typedef struct {
   const void *scores;             /* [seqs][frames][v] */
   const int32_t *tokens;          /* [seqs][frames][given] */
   const int32_t *lengths;         /* [seqs] or NULL */
-  const float *stats;             /* [seqs][frames][2] */
+  const float *maximum;           /* [seqs][frames] */
+  const float *log_sum;           /* [seqs][frames] */
   const float *entropy;           /* [seqs][frames]; may be NULL without grad_entropy */
   const int32_t *top_ids;         /* [seqs][frames][top] */
   const float *grad_logprobs;     /* [seqs][frames][given] or NULL */

@@ -98,14 +98,14 @@ class wfst_loglikes_args(C.Structure):
 
 
 class wfst_token_logprobs_args(C.Structure):
-    _fields_ = ([(n, C.c_void_p) for n in ("scores", "tokens", "lengths", "logprobs", "lse", "entropy", "stats", "top_ids",
-                                           "top_logprobs", "workspace")]
+    _fields_ = ([(n, C.c_void_p) for n in ("scores", "tokens", "lengths", "logprobs", "lse", "entropy", "maximum", "log_sum",
+                                           "top_ids", "top_logprobs", "workspace")]
                 + [(n, C.c_int64) for n in ("workspace_bytes", "seq_stride", "stride")]
                 + [(n, C.c_int32) for n in ("seqs", "frames", "v", "given", "top", "dtype")])
 
 
 class wfst_token_logprobs_backward_args(C.Structure):
-    _fields_ = ([(n, C.c_void_p) for n in ("scores", "tokens", "lengths", "stats", "entropy", "top_ids", "grad_logprobs",
+    _fields_ = ([(n, C.c_void_p) for n in ("scores", "tokens", "lengths", "maximum", "log_sum", "entropy", "top_ids", "grad_logprobs",
                                            "grad_lse", "grad_entropy", "grad_top", "grad_scores")]
                 + [(n, C.c_int64) for n in ("seq_stride", "stride", "grad_seq_stride", "grad_stride")]
                 + [(n, C.c_int32) for n in ("seqs", "frames", "v", "given", "top", "dtype")])
@@ -169,10 +169,8 @@ def load_library():
     lib.wfst_get_lattice.argtypes = [p, i32, p, f32, p, p, i64, p, p, i64, p, p, p]
     lib.wfst_get_lattice_noalloc.argtypes = lib.wfst_get_lattice.argtypes
     lib.wfst_get_lattice_batch.argtypes = [p, p, i32, p, i32, f32, p, p, i64, p, p, i64, p, p, p]
-    lib.wfst_linear.argtypes = [C.POINTER(wfst_linear_args), p]
-    lib.wfst_loglikes.argtypes = [C.POINTER(wfst_loglikes_args), p]
-    lib.wfst_token_logprobs.argtypes = [C.POINTER(wfst_token_logprobs_args), p]
-    lib.wfst_token_logprobs_backward.argtypes = [C.POINTER(wfst_token_logprobs_backward_args), p]
+    for name in ("wfst_linear", "wfst_loglikes", "wfst_token_logprobs", "wfst_token_logprobs_backward"):
+        getattr(lib, name).argtypes = [p, p]             # (an argument struct, or its bytes)
     lib.wfst_token_logprobs_workspace.argtypes = [i64, i32, i32]
     lib.wfst_token_logprobs_workspace.restype = i64
     for name in EXPORTS:

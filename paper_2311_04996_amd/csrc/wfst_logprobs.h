@@ -12,7 +12,7 @@ namespace wfst_ops {
 struct LogprobsArgs {
   const void *scores;
   const int32_t *tokens, *lengths;
-  float *logprobs, *lse, *entropy, *stats;
+  float *logprobs, *lse, *entropy, *maximum, *log_sum;
   int32_t *top_ids;
   float *top_logprobs;
   void *workspace;
@@ -24,7 +24,7 @@ struct LogprobsArgs {
 struct BackwardArgs {
   const void *scores;
   const int32_t *tokens, *lengths;
-  const float *stats, *entropy;
+  const float *maximum, *log_sum, *entropy;
   const int32_t *top_ids;
   const float *grad_logprobs, *grad_lse, *grad_entropy, *grad_top;
   void *grad_scores;
@@ -81,10 +81,11 @@ template <int LANES> __device__ __forceinline__ float sum_over(float v) { return
 template <int LANES> __device__ __forceinline__ int max_over(int v) { return reduce<LANES>(v, [](int a, int b) { return a > b ? a : b; }); }
 template <int LANES> __device__ __forceinline__ int min_over(int v) { return reduce<LANES>(v, [](int a, int b) { return a < b ? a : b; }); }
 
-// what a row's lse, entropy and stats are; one lane writes them
+// what a row's own results are; one lane writes them
 __device__ __forceinline__ void write_row(const LogprobsArgs &a, int64_t row, float m, float sum, float weighted_sum, float ls) {
   if (a.lse) a.lse[row] = m + ls;
-  if (a.stats) { a.stats[2 * row] = m; a.stats[2 * row + 1] = ls; }
+  if (a.maximum) a.maximum[row] = m;
+  if (a.log_sum) a.log_sum[row] = ls;
   if (a.entropy) a.entropy[row] = is_empty(m, ls) ? 0.0f : ls - weighted_sum / sum;
 }
 template <class E>
@@ -416,8 +417,8 @@ __global__ __launch_bounds__(256) void backward_short_kernel(BackwardArgs a) {
     extra[e] = 0.0f;
   }
   Slope r;
-  r.m = a.stats[2 * (int64_t)row];
-  r.ls = a.stats[2 * (int64_t)row + 1];
+  r.m = a.maximum[row];
+  r.ls = a.log_sum[row];
   r.c = a.grad_lse ? a.grad_lse[row] : 0.0f;
   r.gh = a.grad_entropy ? a.grad_entropy[row] : 0.0f;
   r.h = a.grad_entropy ? a.entropy[row] : 0.0f;
@@ -464,8 +465,8 @@ __global__ __launch_bounds__(kLongThreads) void backward_long_kernel(BackwardArg
   }
   for (int i = tid; i < n; i += kLongThreads) ids[i] = named(a, row, i, grads[i]);
   Slope r;
-  r.m = a.stats[2 * (int64_t)row];
-  r.ls = a.stats[2 * (int64_t)row + 1];
+  r.m = a.maximum[row];
+  r.ls = a.log_sum[row];
   r.c = a.grad_lse ? a.grad_lse[row] : 0.0f;
   r.gh = a.grad_entropy ? a.grad_entropy[row] : 0.0f;
   r.h = a.grad_entropy ? a.entropy[row] : 0.0f;

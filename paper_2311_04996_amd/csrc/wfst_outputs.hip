@@ -239,7 +239,7 @@ int32_t wfst_token_logprobs(const wfst_token_logprobs_args *args, void *stream) 
   const int64_t size = type_size(p.dtype), rows = (int64_t)p.seqs * p.frames;
   if (rows > INT_MAX) return refuse(me, "more than 2^31 - 1 rows");
   if (!aligned(p.scores, size) || !aligned(p.tokens, 4) || !aligned(p.lengths, 4) || !aligned(p.logprobs, 4) || !aligned(p.lse, 4) ||
-      !aligned(p.entropy, 4) || !aligned(p.stats, 4) || !aligned(p.top_ids, 4) || !aligned(p.top_logprobs, 4))
+      !aligned(p.entropy, 4) || !aligned(p.maximum, 4) || !aligned(p.log_sum, 4) || !aligned(p.top_ids, 4) || !aligned(p.top_logprobs, 4))
     return refuse(me, "an address is not a multiple of its element's size");
   const int64_t need = wfst_token_logprobs_workspace(rows, p.v, p.top);
   if (need > 0 && (!p.workspace || p.workspace_bytes < need || !aligned(p.workspace, 16)))
@@ -248,16 +248,16 @@ int32_t wfst_token_logprobs(const wfst_token_logprobs_args *args, void *stream) 
   if (ns < 0) return refuse(me, "sizes and strides are too large");
   struct Part { const void *p; int64_t n; };
   const Part read[] = {{p.scores, ns}, {p.tokens, rows * p.given * 4}, {p.lengths, (int64_t)p.seqs * 4}};
-  const Part wrote[] = {{p.given ? p.logprobs : nullptr, rows * p.given * 4}, {p.lse, rows * 4}, {p.entropy, rows * 4}, {p.stats, rows * 8},
+  const Part wrote[] = {{p.given ? p.logprobs : nullptr, rows * p.given * 4}, {p.lse, rows * 4}, {p.entropy, rows * 4}, {p.maximum, rows * 4}, {p.log_sum, rows * 4},
                         {p.top ? p.top_ids : nullptr, rows * p.top * 4}, {p.top ? p.top_logprobs : nullptr, rows * p.top * 4},
                         {p.workspace, need}};
-  for (int i = 0; i < 7; ++i) {
+  for (int i = 0; i < (int)(sizeof(wrote) / sizeof(Part)); ++i) {
     for (const Part &r : read)
       if (overlap(wrote[i].p, wrote[i].n, r.p, r.n)) return refuse(me, "an output overlaps what is read");
     for (int j = 0; j < i; ++j)
       if (overlap(wrote[i].p, wrote[i].n, wrote[j].p, wrote[j].n)) return refuse(me, "two outputs overlap");
   }
-  LogprobsArgs a{p.scores, p.tokens, p.lengths, p.given ? p.logprobs : nullptr, p.lse, p.entropy, p.stats, p.top ? p.top_ids : nullptr,
+  LogprobsArgs a{p.scores, p.tokens, p.lengths, p.given ? p.logprobs : nullptr, p.lse, p.entropy, p.maximum, p.log_sum, p.top ? p.top_ids : nullptr,
                  p.top ? p.top_logprobs : nullptr, p.workspace, p.seq_stride, p.stride, p.seqs, p.frames, p.v, p.given, p.top, 1, 0};
   if (!a.top_ids && !a.top_logprobs) a.top = 0;
   return by_type(p.dtype, [&](auto e) { return run_logprobs<decltype(e)>(a, stream); });
@@ -273,7 +273,7 @@ int32_t wfst_token_logprobs_backward(const wfst_token_logprobs_backward_args *ar
   if (p.given < 0 || p.given > kMaxGiven) return refuse(me, "given must be 0 to 256");
   if (p.top < 0 || p.top > kMaxTop || p.top > p.v) return refuse(me, "top must be 0 to 64, and at most v");
   if (p.seqs == 0 || p.frames == 0) return WFST_OK;
-  if (!p.scores || !p.stats || !p.grad_scores) return refuse(me, "null scores, stats or grad_scores");
+  if (!p.scores || !p.maximum || !p.log_sum || !p.grad_scores) return refuse(me, "null scores, maximum, log_sum or grad_scores");
   if (p.given && p.grad_logprobs && !p.tokens) return refuse(me, "grad_logprobs without tokens");
   if (p.grad_entropy && !p.entropy) return refuse(me, "grad_entropy without entropy");
   if (p.top && p.grad_top && !p.top_ids) return refuse(me, "grad_top without top_ids");
@@ -281,7 +281,7 @@ int32_t wfst_token_logprobs_backward(const wfst_token_logprobs_backward_args *ar
   if (!rows_apart(p.seqs, p.frames, p.v, p.grad_seq_stride, p.grad_stride)) return refuse(me, "the rows of grad_scores overlap");
   const int64_t size = type_size(p.dtype), rows = (int64_t)p.seqs * p.frames;
   if (rows > INT_MAX) return refuse(me, "more than 2^31 - 1 rows");
-  if (!aligned(p.scores, size) || !aligned(p.grad_scores, size) || !aligned(p.tokens, 4) || !aligned(p.lengths, 4) || !aligned(p.stats, 4) ||
+  if (!aligned(p.scores, size) || !aligned(p.grad_scores, size) || !aligned(p.tokens, 4) || !aligned(p.lengths, 4) || !aligned(p.maximum, 4) || !aligned(p.log_sum, 4) ||
       !aligned(p.entropy, 4) || !aligned(p.top_ids, 4) || !aligned(p.grad_logprobs, 4) || !aligned(p.grad_lse, 4) ||
       !aligned(p.grad_entropy, 4) || !aligned(p.grad_top, 4))
     return refuse(me, "an address is not a multiple of its element's size");
@@ -291,12 +291,12 @@ int32_t wfst_token_logprobs_backward(const wfst_token_logprobs_backward_args *ar
   const bool same = p.scores == p.grad_scores && (p.seqs == 1 || p.seq_stride == p.grad_seq_stride) && (p.frames == 1 || p.stride == p.grad_stride);
   if (!same && overlap(p.grad_scores, ng, p.scores, ns)) return refuse(me, "grad_scores overlaps the scores without being them");
   if (overlap(p.grad_scores, ng, p.tokens, rows * p.given * 4) || overlap(p.grad_scores, ng, p.lengths, (int64_t)p.seqs * 4) ||
-      overlap(p.grad_scores, ng, p.stats, rows * 8) || overlap(p.grad_scores, ng, p.entropy, rows * 4) ||
+      overlap(p.grad_scores, ng, p.maximum, rows * 4) || overlap(p.grad_scores, ng, p.log_sum, rows * 4) || overlap(p.grad_scores, ng, p.entropy, rows * 4) ||
       overlap(p.grad_scores, ng, p.top_ids, rows * p.top * 4) || overlap(p.grad_scores, ng, p.grad_logprobs, rows * p.given * 4) ||
       overlap(p.grad_scores, ng, p.grad_lse, rows * 4) || overlap(p.grad_scores, ng, p.grad_entropy, rows * 4) ||
       overlap(p.grad_scores, ng, p.grad_top, rows * p.top * 4))
     return refuse(me, "grad_scores overlaps what is read");
-  BackwardArgs a{p.scores, p.tokens, p.lengths, p.stats, p.entropy, p.top_ids, p.grad_logprobs, p.grad_lse, p.grad_entropy, p.grad_top,
+  BackwardArgs a{p.scores, p.tokens, p.lengths, p.maximum, p.log_sum, p.entropy, p.top_ids, p.grad_logprobs, p.grad_lse, p.grad_entropy, p.grad_top,
                  p.grad_scores, p.seq_stride, p.stride, p.grad_seq_stride, p.grad_stride, p.seqs, p.frames, p.v, p.given, p.top, 1};
   if (!a.grad_logprobs) a.given = 0;
   if (!a.grad_top) a.top = 0;

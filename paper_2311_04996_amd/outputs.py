@@ -9,108 +9,128 @@ take raise ValueError here, what else is wrong with a call raises WfstError.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
+import struct
 from typing import NamedTuple, Optional
 
-from .binding import WFST_OK, WfstError, _on, load_library, wfst_linear_args, wfst_loglikes_args, \
+from .binding import WFST_OK, WfstError, load_library, wfst_linear_args, wfst_loglikes_args, \
     wfst_token_logprobs_args, wfst_token_logprobs_backward_args
 
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
-_types = None
 
 
-def _type_codes():
-    global _types
-    if _types is None:
-        import torch
-        _types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-    return _types
+def _packer(args):
+    """The argument struct as bytes, in one step (filling a ctypes struct costs a small call a tenth of its time)."""
+    letter = {C.c_void_p: "P", C.c_int64: "q", C.c_int32: "i", C.c_float: "f"}
+    return struct.Struct("@" + "".join(letter[t] for _, t in args._fields_))
+
+
+_linear, _loglikes = _packer(wfst_linear_args), _packer(wfst_loglikes_args)
+_logprobs, _backward = _packer(wfst_token_logprobs_args), _packer(wfst_token_logprobs_backward_args)
+torch = lib = _codes = _raw_stream = None
+
+
+def _start():
+    """On the first call: the library, and torch with it."""
+    global torch, lib, _codes, _raw_stream
+    lib = load_library()
+    import torch as t
+    _codes = {t.float32: 0, t.float16: 1, t.bfloat16: 2}
+    _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda dev: t.cuda.current_stream(dev).cuda_stream)
+    torch = t
+
+
+def _device(t, what):
+    if lib is None:
+        _start()
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    return t.get_device()
 
 
 def _code(t, what):
-    c = _type_codes().get(t.dtype)
+    c = _codes.get(t.dtype)
     if c is None:
         raise ValueError(f"{what} must be float32, float16 or bfloat16, not {t.dtype}")
     return c
 
 
-def _same_device(dev, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, not on {dev}")
+def _there(t, dev, what):
+    if t.get_device() != dev:
+        raise ValueError(f"{what} is on {t.device}, not on cuda:{dev}")
 
 
-def _inner(t, what):
-    """The last dimension's elements lie one after the other."""
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError(f"the last dimension of {what} must be contiguous")
-
-
-def _row_stride(t, what):
+def _matrix(t, what):
     """(rows, stride of a row) of a tensor [..., n] whose leading dimensions are one: a matrix, or a view that is like one."""
-    _inner(t, what)
-    if t.dim() == 2:
-        return t.shape[0], t.stride(0)
-    if t.dim() == 1:
-        return 1, t.shape[0]
-    rows, stride = 1, 0
-    for size, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+    st = t.stride()
+    if st[-1] != 1 and t.shape[-1] > 1:
+        raise ValueError(f"the last dimension of {what} must be contiguous")
+    if len(st) == 2:
+        return t.shape[0], st[0]
+    rows, stride = 1, t.shape[-1]
+    for size, s in zip(reversed(t.shape[:-1]), reversed(st[:-1])):
         if size == 1:
             continue
         if rows == 1:
-            stride = st
-        elif st != rows * stride:
-            raise ValueError(f"the leading dimensions of {what} do not merge into one (strides {tuple(t.stride())})")
+            stride = s
+        elif s != rows * stride:
+            raise ValueError(f"the leading dimensions of {what} do not merge into one (strides {tuple(st)})")
         rows *= size
-    return rows, stride if rows > 1 else t.shape[-1]
+    return rows, stride
 
 
 def _grid(t, what):
-    """(sequences, frames, stride of a sequence, stride of a frame) of a tensor [n] / [frames, n] / [sequences, frames, n]."""
-    _inner(t, what)
-    if t.dim() == 3:
-        return t.shape[0], t.shape[1], t.stride(0), t.stride(1)
-    if t.dim() == 2:
-        return 1, t.shape[0], 0, t.stride(0)
-    raise ValueError(f"{what} must have 2 or 3 dimensions, not {t.dim()}")
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
-def _lengths(lengths, seqs, dev):
-    import torch
-    if lengths is None:
-        return
-    if lengths.dtype != torch.int32 or lengths.shape != (seqs,) or not lengths.is_contiguous():
-        raise ValueError(f"lengths must be a contiguous int32 tensor of {seqs} entries")
-    _same_device(dev, lengths=lengths)
+    """(sequences, frames, stride of a sequence, stride of a frame) of a tensor [frames, n] or [sequences, frames, n]."""
+    st, n = t.stride(), t.dim()
+    if n != 2 and n != 3:
+        raise ValueError(f"{what} must have 2 or 3 dimensions, not {n}")
+    if st[-1] != 1 and t.shape[-1] > 1:
+        raise ValueError(f"the last dimension of {what} must be contiguous")
+    return (t.shape[0], t.shape[1], st[0], st[1]) if n == 3 else (1, t.shape[0], 0, st[0])
 
 
 def _dense(t, shape, dtype, what, dev):
+    """Address of a contiguous tensor of this shape and type, 0 if there is none."""
     if t is None:
-        return
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        return 0
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
-    _same_device(dev, **{what: t})
+    _there(t, dev, what)
+    return t.data_ptr()
 
 
-def _cuda(t, what):
-    if not t.is_cuda:
-        raise ValueError(f"{what} must be a CUDA tensor")
+def _vector(t, n, what, dev):
+    """(address, type) of a contiguous vector of n values of any type."""
+    if t is None:
+        return 0, 0
+    if t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous tensor of {n} entries")
+    _there(t, dev, what)
+    return t.data_ptr(), _code(t, what)
+
+
+def _new(make, shape, dtype, dev, stream):
+    """A new tensor, allocated (and filled) on the stream that the kernel runs on."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=dev)
 
 
 def _run(entry, args, dev, stream):
-    import torch
-    s = torch.cuda.current_stream(dev) if stream is None else stream
-    if s.device != dev:
-        raise ValueError(f"the stream is on {s.device}, the tensors on {dev}")
-    with contextlib.nullcontext() if torch.cuda.current_device() == dev.index else torch.cuda.device(dev):
-        rc = entry(C.byref(args), s.cuda_stream)
+    if stream is not None:
+        if stream.device.index != dev:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{dev}")
+        raw = stream.cuda_stream
+    else:
+        raw = _raw_stream(dev)
+    if torch.cuda.current_device() == dev:
+        rc = entry(args, raw)
+    else:
+        with torch.cuda.device(dev):
+            rc = entry(args, raw)
     if rc != WFST_OK:
-        raise WfstError(rc, load_library().wfst_last_error(None).decode())
+        raise WfstError(rc, lib.wfst_last_error(None).decode())
 
 
 def linear(x, weight, bias=None, activation=None, residual=None, scale=1.0, out=None, out_dtype=None, stream=None):
@@ -120,37 +140,38 @@ def linear(x, weight, bias=None, activation=None, residual=None, scale=1.0, out=
     bias: [n], any of the types.  activation: None, "relu", "silu" or "gelu" (with erf).  residual: [..., n] of the
     result's type.  out: where the result goes, [..., n]; it may be `residual` itself.  out_dtype: the
     result's type without `out` (default x's)."""
-    import torch
-    _cuda(x, "x")
-    dev = x.device
-    if x.dim() < 1 or weight.dim() != 2 or x.shape[-1] != weight.shape[1]:
-        raise ValueError(f"x {tuple(x.shape)} and weight {tuple(weight.shape)} do not fit")
+    dev = _device(x, "x")
+    shape = x.shape
+    if x.dim() < 1 or weight.dim() != 2 or shape[-1] != weight.shape[1]:
+        raise ValueError(f"x {tuple(shape)} and weight {tuple(weight.shape)} do not fit")
     if weight.dtype != x.dtype:
         raise ValueError(f"weight is {weight.dtype}, x is {x.dtype}")
-    if activation not in ACTIVATIONS:
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError(f"unknown activation {activation!r}")
-    n = weight.shape[0]
-    shape = (*x.shape[:-1], n)
-    _same_device(dev, weight=weight, bias=bias, residual=residual, out=out)
-    _inner(weight, "weight")
-    if bias is not None and (tuple(bias.shape) != (n,) or (n > 1 and bias.stride(0) != 1)):
-        raise ValueError(f"bias must be a contiguous tensor of {n} entries")
+    n, k = weight.shape
+    shape = (*shape[:-1], n)
+    code = _code(x, "x")
+    _there(weight, dev, "weight")
+    ws = _matrix(weight, "weight")[1]
+    b, b_code = _vector(bias, n, "bias", dev)
+    rows, xs = _matrix(x, "x")
     if out is None:
-        with _on(stream):
-            out = torch.empty(shape, dtype=x.dtype if out_dtype is None else out_dtype, device=dev)
-    elif tuple(out.shape) != shape or (out_dtype is not None and out.dtype != out_dtype):
-        raise ValueError(f"out is {out.dtype} {tuple(out.shape)}, the result {out_dtype or out.dtype} {shape}")
-    rows, xs = _row_stride(x, "x")
-    _, ys = _row_stride(out, "out")
-    rs = 0
+        out = _new(torch.empty, shape, x.dtype if out_dtype is None else out_dtype, x.device, stream)
+        ys = n
+    else:
+        if out.shape != shape or (out_dtype is not None and out.dtype != out_dtype):
+            raise ValueError(f"out is {out.dtype} {tuple(out.shape)}, the result {out_dtype or out.dtype} {shape}")
+        _there(out, dev, "out")
+        ys = _matrix(out, "out")[1]
+    r = rs = 0
     if residual is not None:
-        if tuple(residual.shape) != shape or residual.dtype != out.dtype:
+        if residual.shape != shape or residual.dtype != out.dtype:
             raise ValueError(f"residual is {residual.dtype} {tuple(residual.shape)}, the result {out.dtype} {shape}")
-        rs = _row_stride(residual, "residual")[1]
-    args = wfst_linear_args(x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(residual), out.data_ptr(), rows, xs, weight.stride(0), rs, ys,
-                            x.shape[-1], n, _code(x, "x"), 0 if bias is None else _code(bias, "bias"), _code(out, "out"),
-                            ACTIVATIONS[activation], float(scale))
-    _run(load_library().wfst_linear, args, dev, stream)
+        _there(residual, dev, "residual")
+        r, rs = residual.data_ptr(), _matrix(residual, "residual")[1]
+    _run(lib.wfst_linear, _linear.pack(x.data_ptr(), weight.data_ptr(), b, r, out.data_ptr(), rows, xs, ws, rs, ys, k, n, code, b_code,
+                                       _code(out, "out"), act, scale), dev, stream)
     return out
 
 
@@ -162,32 +183,28 @@ def loglikes(hidden, weight, bias=None, log_prior=None, lengths=None, out=None, 
     given transposed); weight: [v, k] of hidden's type, v <= 2048; bias: [v]; log_prior: float32 [v].
     lengths: int32 CUDA tensor [sequences]: frames behind a sequence's length are not computed, and what `out` holds
     there stays (without `out` they are 0).  out_dtype: the result's type without `out` (default float32)."""
-    import torch
-    _cuda(hidden, "hidden")
-    dev = hidden.device
-    if weight.dim() != 2 or hidden.dim() not in (2, 3) or hidden.shape[-1] != weight.shape[1]:
+    dev = _device(hidden, "hidden")
+    if weight.dim() != 2 or hidden.dim() < 1 or hidden.shape[-1] != weight.shape[1]:
         raise ValueError(f"hidden {tuple(hidden.shape)} and weight {tuple(weight.shape)} do not fit")
     if weight.dtype != hidden.dtype:
         raise ValueError(f"weight is {weight.dtype}, hidden is {hidden.dtype}")
-    v = weight.shape[0]
+    v, k = weight.shape
     shape = (*hidden.shape[:-1], v)
-    _same_device(dev, weight=weight, bias=bias, out=out)
-    _inner(weight, "weight")
-    if bias is not None and (tuple(bias.shape) != (v,) or (v > 1 and bias.stride(0) != 1)):
-        raise ValueError(f"bias must be a contiguous tensor of {v} entries")
-    _dense(log_prior, (v,), torch.float32, "log_prior", dev)
+    code = _code(hidden, "hidden")
+    _there(weight, dev, "weight")
+    ws = _matrix(weight, "weight")[1]
+    b, b_code = _vector(bias, v, "bias", dev)
+    prior = _dense(log_prior, (v,), torch.float32, "log_prior", dev)
     seqs, frames, xss, xs = _grid(hidden, "hidden")
-    _lengths(lengths, seqs, dev)
+    le = _dense(lengths, (seqs,), torch.int32, "lengths", dev)
     if out is None:
-        with _on(stream):
-            out = (torch.empty if lengths is None else torch.zeros)(shape, dtype=out_dtype or torch.float32, device=dev)
-    elif tuple(out.shape) != shape or (out_dtype is not None and out.dtype != out_dtype):
+        out = _new(torch.empty if lengths is None else torch.zeros, shape, out_dtype or torch.float32, hidden.device, stream)
+    elif out.shape != shape or (out_dtype is not None and out.dtype != out_dtype):
         raise ValueError(f"out is {out.dtype} {tuple(out.shape)}, the result {out_dtype or out.dtype} {shape}")
+    _there(out, dev, "out")
     _, _, oss, os_ = _grid(out, "out")
-    args = wfst_loglikes_args(hidden.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(log_prior), _ptr(lengths), out.data_ptr(),
-                              xss, xs, weight.stride(0), oss, os_, seqs, frames, hidden.shape[-1], v,
-                              _code(hidden, "hidden"), 0 if bias is None else _code(bias, "bias"), _code(out, "out"))
-    _run(load_library().wfst_loglikes, args, dev, stream)
+    _run(lib.wfst_loglikes, _loglikes.pack(hidden.data_ptr(), weight.data_ptr(), b, prior, le, out.data_ptr(), xss, xs, ws, oss, os_,
+                                           seqs, frames, k, v, code, b_code, _code(out, "out")), dev, stream)
     return out
 
 
@@ -196,7 +213,8 @@ class TokenLogprobs(NamedTuple):
     logprobs: Optional[object]       # [..., given]
     lse: object                      # [...]
     entropy: object                  # [...]
-    stats: object                    # [..., 2]: the row's maximum, and the log of its sum of e^(score - maximum)
+    maximum: object                  # [...]: the row's maximum,
+    log_sum: object                  # [...]: and the log of its sum of e^(score - maximum): what the gradient needs
     top_ids: Optional[object]        # [..., top]
     top_logprobs: Optional[object]   # [..., top]
 
@@ -206,34 +224,39 @@ def token_logprobs(scores, tokens=None, top=0, lengths=None, stream=None):
     (wfst_token_logprobs).
 
     scores: [rows, v] or [sequences, frames, v] logits or log-likelihoods, float32, float16 or bfloat16, any strides of
-    the first dimensions.  tokens: int32 [..., given] (or [...], one per row), -1 for none.  top: 0 to 64.
+    the first dimensions.  tokens: int32 [..., given] (or [...], one per row), -1 for none; at most 256 per row.  top: 0 to 64.
     lengths: int32 CUDA tensor [sequences]: rows behind a sequence's length are not read, their results are 0.
     A row that rules everything out (-inf) has lse -inf, log-probabilities -inf and entropy 0."""
-    import torch
-    _cuda(scores, "scores")
-    dev = scores.device
+    dev = _device(scores, "scores")
+    code = _code(scores, "scores")
     seqs, frames, ss, st = _grid(scores, "scores")
-    lead, v = tuple(scores.shape[:-1]), scores.shape[-1]
-    _lengths(lengths, seqs, dev)
-    given = 0
+    lead, v = scores.shape[:-1], scores.shape[-1]
+    le = _dense(lengths, (seqs,), torch.int32, "lengths", dev)
+    new = torch.empty if lengths is None else torch.zeros
+    f32, i32, on = torch.float32, torch.int32, scores.device
+    given = tok = lp_at = ids_at = tlp_at = ws_at = 0
+    lp = ids = tlp = ws = None
     if tokens is not None:
-        given = 1 if tokens.dim() == len(lead) else tokens.shape[-1]
-        _dense(tokens, lead if tokens.dim() == len(lead) else (*lead, given), torch.int32, "tokens", dev)
-    top = int(top)
-    lib = load_library()
-    with _on(stream):
-        new = torch.empty if lengths is None else torch.zeros
-        lp = new(tuple(tokens.shape), dtype=torch.float32, device=dev) if tokens is not None else None
-        lse, ent = new(lead, dtype=torch.float32, device=dev), new(lead, dtype=torch.float32, device=dev)
-        stats = new((*lead, 2), dtype=torch.float32, device=dev)
-        ids = new((*lead, top), dtype=torch.int32, device=dev) if top > 0 else None
-        tlp = new((*lead, top), dtype=torch.float32, device=dev) if top > 0 else None
-        need = lib.wfst_token_logprobs_workspace(seqs * frames, v, top)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
-    args = wfst_token_logprobs_args(scores.data_ptr(), _ptr(tokens), _ptr(lengths), _ptr(lp), lse.data_ptr(), ent.data_ptr(), stats.data_ptr(),
-                                    _ptr(ids), _ptr(tlp), _ptr(ws), max(need, 0), ss, st, seqs, frames, v, given, top, _code(scores, "scores"))
-    _run(lib.wfst_token_logprobs, args, dev, stream)
-    return TokenLogprobs(lp, lse, ent, stats, ids, tlp)
+        if tokens.dim() == len(lead):
+            given, shape = 1, lead
+        else:
+            given = tokens.shape[-1]
+            shape = (*lead, given)
+        tok = _dense(tokens, shape, i32, "tokens", dev)
+        lp = _new(new, shape, f32, on, stream)
+        lp_at = lp.data_ptr()
+    lse, entropy, maximum, log_sum = _new(new, (4, *lead), f32, on, stream).unbind(0)
+    if top > 0:
+        ids, tlp = _new(new, (*lead, top), i32, on, stream), _new(new, (*lead, top), f32, on, stream)
+        ids_at, tlp_at = ids.data_ptr(), tlp.data_ptr()
+    need = lib.wfst_token_logprobs_workspace(seqs * frames, v, top)
+    if need > 0:
+        ws = _new(torch.empty, need, torch.uint8, on, stream)
+        ws_at = ws.data_ptr()
+    _run(lib.wfst_token_logprobs, _logprobs.pack(scores.data_ptr(), tok, le, lp_at, lse.data_ptr(), entropy.data_ptr(), maximum.data_ptr(),
+                                                 log_sum.data_ptr(), ids_at, tlp_at, ws_at, need, ss, st, seqs, frames, v, given, top, code),
+         dev, stream)
+    return TokenLogprobs(lp, lse, entropy, maximum, log_sum, ids, tlp)
 
 
 def token_logprobs_backward(scores, result, tokens=None, grad_logprobs=None, grad_lse=None, grad_entropy=None, grad_top=None,
@@ -243,38 +266,34 @@ def token_logprobs_backward(scores, result, tokens=None, grad_logprobs=None, gra
     scores, tokens, lengths: as the forward call had them; result: what it returned.  grad_*: float32 gradients of
     result.logprobs, .lse, .entropy and .top_logprobs (None: 0).  Returns the gradient in the scores' type and shape; out
     may be the scores themselves.  Rows behind a sequence's length are not computed (0 without `out`)."""
-    import torch
-    _cuda(scores, "scores")
-    dev = scores.device
+    dev = _device(scores, "scores")
+    code = _code(scores, "scores")
     seqs, frames, ss, st = _grid(scores, "scores")
-    lead, v = tuple(scores.shape[:-1]), scores.shape[-1]
-    _lengths(lengths, seqs, dev)
-    given, top = 0, 0
-    if tokens is not None:
+    lead, v = scores.shape[:-1], scores.shape[-1]
+    f32 = torch.float32
+    le = _dense(lengths, (seqs,), torch.int32, "lengths", dev)
+    given = top = tok = gl = ids = gt = 0
+    if grad_logprobs is not None:
+        if tokens is None:
+            raise ValueError("grad_logprobs without tokens")
         given = 1 if tokens.dim() == len(lead) else tokens.shape[-1]
-        _dense(tokens, lead if tokens.dim() == len(lead) else (*lead, given), torch.int32, "tokens", dev)
-        _dense(grad_logprobs, tokens.shape, torch.float32, "grad_logprobs", dev)
-    elif grad_logprobs is not None:
-        raise ValueError("grad_logprobs without tokens")
+        tok = _dense(tokens, lead if tokens.dim() == len(lead) else (*lead, given), torch.int32, "tokens", dev)
+        gl = _dense(grad_logprobs, tokens.shape, f32, "grad_logprobs", dev)
     if grad_top is not None:
         if result.top_ids is None:
             raise ValueError("grad_top, but the result has no top alternatives")
         top = result.top_ids.shape[-1]
-        _dense(result.top_ids, (*lead, top), torch.int32, "top_ids", dev)
-        _dense(grad_top, (*lead, top), torch.float32, "grad_top", dev)
-    _dense(result.stats, (*lead, 2), torch.float32, "stats", dev)
-    _dense(result.entropy, lead, torch.float32, "entropy", dev)
-    _dense(grad_lse, lead, torch.float32, "grad_lse", dev)
-    _dense(grad_entropy, lead, torch.float32, "grad_entropy", dev)
+        ids = _dense(result.top_ids, (*lead, top), torch.int32, "top_ids", dev)
+        gt = _dense(grad_top, (*lead, top), f32, "grad_top", dev)
+    m, ls = _dense(result.maximum, lead, f32, "maximum", dev), _dense(result.log_sum, lead, f32, "log_sum", dev)
+    gs, gh = _dense(grad_lse, lead, f32, "grad_lse", dev), _dense(grad_entropy, lead, f32, "grad_entropy", dev)
+    h = _dense(result.entropy, lead, f32, "entropy", dev) if gh else 0
     if out is None:
-        with _on(stream):
-            out = (torch.empty if lengths is None else torch.zeros)(tuple(scores.shape), dtype=scores.dtype, device=dev)
-    elif out.shape != scores.shape or out.dtype != scores.dtype or out.device != dev:
-        raise ValueError(f"out must be a {scores.dtype} tensor {tuple(scores.shape)} on {dev}")
-    _, _, gs, gt = _grid(out, "out")
-    args = wfst_token_logprobs_backward_args(
-        scores.data_ptr(), _ptr(tokens), _ptr(lengths), result.stats.data_ptr(), result.entropy.data_ptr(),
-        _ptr(result.top_ids) if top else None, _ptr(grad_logprobs), _ptr(grad_lse), _ptr(grad_entropy), _ptr(grad_top), out.data_ptr(),
-        ss, st, gs, gt, seqs, frames, v, given, top, _code(scores, "scores"))
-    _run(load_library().wfst_token_logprobs_backward, args, dev, stream)
+        out = _new(torch.empty if lengths is None else torch.zeros, scores.shape, scores.dtype, scores.device, stream)
+    elif out.shape != scores.shape or out.dtype != scores.dtype:
+        raise ValueError(f"out must be a {scores.dtype} tensor {tuple(scores.shape)}")
+    _there(out, dev, "out")
+    _, _, oss, ost = _grid(out, "out")
+    _run(lib.wfst_token_logprobs_backward, _backward.pack(scores.data_ptr(), tok, le, m, ls, h, ids, gl, gs, gh, gt, out.data_ptr(), ss, st, oss, ost,
+                                                          seqs, frames, v, given, top, code), dev, stream)
     return out

@@ -71,7 +71,7 @@ def test_loglikes_refuses(lib, kw, word):
 
 
 def tlp(**kw):
-    d = dict(scores=1 * A, tokens=2 * A, lengths=3 * A, logprobs=4 * A, lse=5 * A, entropy=6 * A, stats=10 * A, top_ids=7 * A, top_logprobs=8 * A,
+    d = dict(scores=1 * A, tokens=2 * A, lengths=3 * A, logprobs=4 * A, lse=5 * A, entropy=6 * A, maximum=10 * A, log_sum=11 * A, top_ids=7 * A, top_logprobs=8 * A,
              workspace=9 * A, workspace_bytes=1 << 30, seq_stride=290, stride=29, seqs=3, frames=10, v=29, given=2, top=4, dtype=1)
     d.update(kw)
     return b.wfst_token_logprobs_args(**d)
@@ -84,7 +84,7 @@ def tlp(**kw):
     (dict(scores=A + 1), "multiple"), (dict(tokens=2 * A + 2), "multiple"), (dict(lse=5 * A + 2), "multiple"), (dict(top_ids=7 * A + 1), "multiple"),
     (dict(seq_stride=1 << 62), "large"), (dict(seqs=1 << 17, frames=1 << 17), "rows"),
     (dict(lse=A), "overlaps what is read"), (dict(entropy=2 * A + 4), "overlaps what is read"), (dict(logprobs=3 * A + 8), "overlaps what is read"),
-    (dict(entropy=5 * A + 4), "two outputs"), (dict(stats=6 * A), "two outputs"), (dict(stats=10 * A + 2), "multiple"), (dict(top_logprobs=7 * A), "two outputs"),
+    (dict(entropy=5 * A + 4), "two outputs"), (dict(maximum=6 * A), "two outputs"), (dict(log_sum=10 * A), "two outputs"), (dict(maximum=10 * A + 2), "multiple"), (dict(top_logprobs=7 * A), "two outputs"),
 ])
 def test_token_logprobs_refuses(lib, kw, word):
     refused(lib, "wfst_token_logprobs", tlp(**kw), word)
@@ -105,7 +105,7 @@ def test_token_logprobs_needs_its_workspace(lib):
 
 
 def bwd(**kw):
-    d = dict(scores=1 * A, tokens=2 * A, lengths=3 * A, stats=4 * A, entropy=5 * A, top_ids=6 * A, grad_logprobs=7 * A, grad_lse=8 * A,
+    d = dict(scores=1 * A, tokens=2 * A, lengths=3 * A, maximum=4 * A, log_sum=12 * A, entropy=5 * A, top_ids=6 * A, grad_logprobs=7 * A, grad_lse=8 * A,
              grad_entropy=9 * A, grad_top=10 * A, grad_scores=11 * A, seq_stride=290, stride=29, grad_seq_stride=290, grad_stride=29,
              seqs=3, frames=10, v=29, given=2, top=4, dtype=0)
     d.update(kw)
@@ -114,12 +114,12 @@ def bwd(**kw):
 
 @pytest.mark.parametrize("kw, word", [
     (dict(dtype=3), "type"), (dict(seqs=-1), "seqs"), (dict(v=0), "2^30"), (dict(given=257), "256"), (dict(top=65), "64"),
-    (dict(scores=None), "null"), (dict(stats=None), "null"), (dict(grad_scores=None), "null"), (dict(tokens=None), "without tokens"),
+    (dict(scores=None), "null"), (dict(maximum=None), "null"), (dict(log_sum=None), "null"), (dict(grad_scores=None), "null"), (dict(tokens=None), "without tokens"),
     (dict(entropy=None), "without entropy"), (dict(top_ids=None), "without top_ids"), (dict(stride=-1), "stride"),
     (dict(grad_stride=28), "rows of grad_scores"), (dict(grad_seq_stride=100), "rows of grad_scores"), (dict(grad_scores=11 * A + 2), "multiple"),
     (dict(grad_top=10 * A + 1), "multiple"), (dict(seq_stride=1 << 62), "large"), (dict(grad_scores=A + 4), "scores without being them"),
     (dict(grad_scores=A, grad_stride=30, grad_seq_stride=300), "scores without being them"),
-    (dict(grad_scores=2 * A), "overlaps what is read"), (dict(grad_scores=4 * A), "overlaps what is read"),
+    (dict(grad_scores=2 * A), "overlaps what is read"), (dict(grad_scores=4 * A), "overlaps what is read"), (dict(grad_scores=12 * A - 8), "overlaps what is read"),
     (dict(grad_scores=10 * A + 8), "overlaps what is read"),
 ])
 def test_token_logprobs_backward_refuses(lib, kw, word):
@@ -134,7 +134,7 @@ def test_null_arguments_and_empty_calls(lib):
     assert lib.wfst_loglikes(C.byref(llk(seqs=0, x=None, out=None)), None) == OK
     assert lib.wfst_loglikes(C.byref(llk(frames=0, x=None, out=None)), None) == OK
     assert lib.wfst_token_logprobs(C.byref(tlp(frames=0, scores=None, tokens=None)), None) == OK
-    assert lib.wfst_token_logprobs_backward(C.byref(bwd(seqs=0, scores=None, stats=None, grad_scores=None)), None) == OK
+    assert lib.wfst_token_logprobs_backward(C.byref(bwd(seqs=0, scores=None, maximum=None, grad_scores=None)), None) == OK
 
 
 def test_the_message_belongs_to_the_thread_that_made_the_call(lib):
@@ -171,6 +171,12 @@ def test_argument_structs_are_laid_out_as_in_the_header(tmp_path):
     src.write_text("\n".join(lines + ["  return 0;", "}"]))
     subprocess.check_call(["gcc", "-std=c99", "-Wall", "-Werror", "-I" + os.path.join(root, "include"), str(src), "-o", str(exe)])
     assert [int(x) for x in subprocess.check_output([str(exe)]).split()] == want
+    from paper_2311_04996_amd import outputs
+    for s in structs:                                      # the struct as the Python functions pack it
+        t = getattr(b, s)
+        n = len(t._fields_)
+        a = t.from_buffer_copy(outputs._packer(t).pack(*range(1, n + 1)).ljust(C.sizeof(t), b"\0"))
+        assert [int(getattr(a, name)) for name, _ in t._fields_] == list(range(1, n + 1))
 
 
 def test_cpu_tensors_are_refused():
