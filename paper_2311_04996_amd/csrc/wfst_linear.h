@@ -166,57 +166,54 @@ template <class E> __device__ __forceinline__ i32x4 chunk_of(const char *row, in
   return c;
 }
 
-// A tile of BM rows of x by BN rows of w, WM x WN of them per wave.  LDS holds 2 or 3 parts of ROW bytes of k of each row, at
-// chunk c ^ swizzle(row): the 16 lanes that read a column of chunks together are then in different banks.
-template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES = 3>
+// A tile of BM rows of x by GROUPS times BN rows of w, WM x WN of each group per wave.  Its product goes by parts: ROW bytes of k of the
+// rows of x and of one group of w, the groups in turn.  LDS holds STAGES parts, chunk c of a row at c ^ swizzle(row): the 16
+// lanes that read a column of chunks together are then in different banks.
+template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES = 3, int GROUPS = 1>
 struct Tile {
   static constexpr int kWavesM = BM / WM, kWavesN = BN / WN, kWaves = kWavesM * kWavesN, kThreads = 64 * kWaves;
-  static constexpr int kChunks = ROW / 16;
+  static constexpr int kChunks = ROW / 16, kSteps = kChunks / 2;
   static constexpr int kStage = (BM + BN) * ROW, kPieces = kStage / 1024;      // 1024 bytes per wave and load
   static constexpr int kLoads = (kPieces + kWaves - 1) / kWaves;
   static constexpr int kTM = WM / 32, kTN = WN / 32;
   static_assert(kStage % 1024 == 0 && BM % (64 / kChunks) == 0 && WM % 32 == 0 && WN % 32 == 0, "whole loads, of x or of w");
-  static_assert((ROW == 64 || ROW == 128 || (ROW == 32 && STAGES == 2)) && (STAGES == 2 || STAGES == 3), "as part() takes them");
+  static_assert((ROW == 64 || ROW == 128) && STAGES >= 2 && STAGES <= 4, "an even number of steps; stages as the kernels have them");
+  // parts in a row whose stage and group are the same again behind them
+  static constexpr int kTurn = STAGES % GROUPS == 0 ? STAGES : GROUPS % STAGES == 0 ? GROUPS : STAGES == 4 && GROUPS == 2 ? 4 : STAGES * GROUPS;
+  typedef f32x16 Sums[GROUPS][kTN][kTM];
 
-  static __device__ __forceinline__ int swizzle(int row) { return ROW == 32 ? (row >> 3) & 1 : ROW == 64 ? (row >> 2) & 3 : (row >> 1) & 7; }
+  static __device__ __forceinline__ int swizzle(int row) { return ROW == 64 ? (row >> 2) & 3 : (row >> 1) & 7; }
 
-  // Piece i of this wave: 1024 bytes of a stage, 64 / kChunks rows of it.  Row r of the tile is x's row r for r < BM, w's row r - BM behind
-  // that; a piece is of one of them.  (If the waves do not share them out evenly, some load the last piece again.)
+  // Piece i of this wave: 1024 bytes of a stage, 64 / kChunks rows of it.  Row r of a part is x's row r for r < BM, row r - BM of the
+  // group of w behind that; a piece is of one of them.  (If the waves do not share them out evenly, some load the last piece again.)
   static __device__ __forceinline__ int piece(int i) {
     const int n = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) + kWaves * i;
     return kPieces % kWaves != 0 && n >= kPieces ? kPieces - 1 : n;
   }
+  static __device__ __forceinline__ bool piece_of_x(int i) { return piece(i) * (64 / kChunks) < BM; }
   static __device__ __forceinline__ int piece_row(int i) { return piece(i) * (64 / kChunks) + (threadIdx.x & 63) / kChunks; }
   static __device__ __forceinline__ int piece_chunk(int i) { return ((threadIdx.x & 63) % kChunks) ^ swizzle(piece_row(i)); }
 
-  // Where this lane's chunks of the pieces lie behind the start of x or w, in bytes.
-  int at[kLoads];
-  // offset_of(r): of row r of the tile.  A row behind the end may be any other one, or lie out of bounds
-  template <class OffsetOf> __device__ __forceinline__ void aim(OffsetOf offset_of) {
+  // Where this lane's chunks of the pieces lie behind the start of x or w, in bytes; a group of w behind the one before it.
+  int at[kLoads], group_bytes;
+  // offset_of(r): of row r of the first group's parts.  A row behind the end may be any other one, or lie out of bounds.
+  template <class OffsetOf> __device__ __forceinline__ void aim(OffsetOf offset_of, int bytes) {
+    group_bytes = bytes;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) at[i] = offset_of(piece_row(i)) + piece_chunk(i) * 16;
   }
-  // Part `part` of k on its way into `stage`, without a register between.  Chunks behind the end of a row are whatever lies
-  // there, or nothing if that is out of bounds: they are put to zero where they are used.
-  __device__ __forceinline__ void load(Buffer x, Buffer w, char *stage, int part) const {
+  // Part `k` of k and group `h` on its way into `stage`, without a register between.  Chunks behind the end of a row are whatever
+  // lies there, or nothing if that is out of bounds (all of the offset is held against the end): they are put to zero where
+  // they are used.
+  __device__ __forceinline__ void load(Buffer x, Buffer w, char *stage, int k, int h) const {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(piece(i) * (64 / kChunks) < BM ? x : w,
-                                               (__attribute__((address_space(3))) void *)(stage + piece(i) * 1024), 16, at[i], part * ROW, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(piece_of_x(i) ? x : w, (__attribute__((address_space(3))) void *)(stage + piece(i) * 1024), 16,
+                                               at[i] + (k * ROW + (GROUPS > 1 && !piece_of_x(i) ? h * group_bytes : 0)), 0, 0, 0);
   }
-  // The same by way of registers, for rows whose chunks are no multiples of 16 bytes in memory (a 16-byte load may start
-  // anywhere) or end inside one; what is behind the end of a row is zero.
-  static __device__ __forceinline__ void fetch(i32x4 (&reg)[kLoads], const char *const (&from)[kLoads], int part, int k_bytes) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) reg[i] = chunk_of<E>(from[i], part * ROW + piece_chunk(i) * 16, k_bytes);
-  }
-  static __device__ __forceinline__ void put(char *stage, const i32x4 (&reg)[kLoads]) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<i32x4 *>(stage + piece(i) * 1024 + (threadIdx.x & 63) * 16) = reg[i];
-  }
+
   // What a wave multiplies in one step: 16 bytes of k per lane, half of the wave each of two neighbouring chunks.
   struct Step { i32x4 w[kTN], x[kTM]; };
-  static constexpr int kSteps = kChunks / 2;
   static __device__ __forceinline__ void read(Step &f, const char *stage, int step) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = 2 * step + (lane >> 5);
     const int m0 = (wave / kWavesN) * WM + (lane & 31), n0 = BM + (wave % kWavesN) * WN + (lane & 31);
@@ -232,107 +229,104 @@ struct Tile {
 #pragma unroll
       for (int j = 0; j < kTM; ++j) acc[i][j] = Mma<E>::run(f.w[i], f.x[j], acc[i][j]);
   }
-  // The same at the end of k, `left` bytes of which are left at the part's start: what is behind them counts as zero, in x and
-  // in w (it may be NaN in either).
-  static __device__ __forceinline__ void multiply_last(Step &f, int step, int left, f32x16 (&acc)[kTN][kTM]) {
+  // `left` bytes of k are left at the part's start: what is behind them counts as zero, in x and in w (it may be NaN in either).
+  static __device__ __forceinline__ void cut(Step &f, int step, int left) {
     if ((2 * step + ((threadIdx.x & 63) >> 5)) * 16 >= left) {
 #pragma unroll
       for (int i = 0; i < kTN; ++i) f.w[i] = i32x4{0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < kTM; ++i) f.x[i] = i32x4{0, 0, 0, 0};
     }
-    multiply(f, acc);
   }
-  // One part but the last, from stage `here`: the next step's chunks are read while a step is multiplied, across the parts too.
-  // Before the last step the waves meet: the part behind has arrived in `next` then, and nobody reads `here` any more, so
-  // that the part STAGES further on can come there.  F: where the part's first step is in f.
-  template <int F>
-  __device__ __forceinline__ void part(int p, Buffer x, Buffer w, char *here, char *next, Step (&f)[2], f32x16 (&acc)[kTN][kTM], bool used) {
+  // Part I of a turn that begins at part k of k.  The next step's chunks are read while a step is multiplied, across the parts too:
+  // before the last step the waves meet; the part behind has arrived then, and nobody reads this one's stage any more, so that
+  // the part STAGES further on can come there.
+  template <int I, bool LAST>
+  __device__ __forceinline__ void part(int k, int k_bytes, Buffer x, Buffer w, char *const (&stage)[STAGES], Step (&f)[2], Sums &acc, unsigned used) {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       if (s + 1 < kSteps) {
-        read(f[(F + s + 1) & 1], here, s + 1);
+        read(f[(s + 1) & 1], stage[I % STAGES], s + 1);
       } else {
         wait_loads<(STAGES - 2) * kLoads>();
         meet();
-        read(f[(F + s + 1) & 1], next, 0);
+        read(f[0], stage[(I + 1) % STAGES], 0);
         __builtin_amdgcn_sched_barrier(0);
-        load(x, w, here, p + STAGES);
+        load(x, w, stage[I % STAGES], k + (I + STAGES) / GROUPS, (I + STAGES) % GROUPS);
       }
       __builtin_amdgcn_sched_barrier(0);             // the reads go out before the products that hide them
-      if (used) multiply(f[(F + s) & 1], acc);
+      if (LAST) cut(f[s & 1], s, k_bytes - (k + I / GROUPS) * ROW);
+      if (GROUPS == 1 || (used >> (I % GROUPS) & 1)) multiply(f[s & 1], acc[I % GROUPS]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
+  template <int I, bool LAST>
+  __device__ __forceinline__ void turn(int k, int parts, int k_bytes, Buffer x, Buffer w, char *const (&stage)[STAGES], Step (&f)[2], Sums &acc, unsigned used) {
+    if constexpr (I < kTurn) {
+      if (!LAST || k * GROUPS + I < parts * GROUPS) part<I, LAST>(k, k_bytes, x, w, stage, f, acc, used);
+      turn<I + 1, LAST>(k, parts, k_bytes, x, w, stage, f, acc, used);
+    }
+  }
   // The whole product.  Ends with all waves done with LDS.  (STAGES parts behind the last one are loaded too, while the last ones
-  // are multiplied, and not used: so every wait has the same number of loads behind it.)  used: whether this wave's sums are.
-  __device__ __forceinline__ void product(Buffer x, Buffer w, char *s0, char *s1, char *s2, int k_bytes, f32x16 (&acc)[kTN][kTM], bool used = true) {
-    constexpr int kFlip = kSteps & 1;                // one step per part: the two of f take turns
+  // are multiplied, and not used: so every wait has the same number of loads behind it.)  used: a bit per group, whether this
+  // wave's sums of it are (uniform).
+  __device__ __forceinline__ void product(Buffer x, Buffer w, char *const (&stage)[STAGES], int k_bytes, Sums &acc, unsigned used = ~0u) {
+    static_assert(kTurn % GROUPS == 0 && kTurn % STAGES == 0, "a turn ends where it began");
+    constexpr int kStep = kTurn / GROUPS;            // parts of k in a turn
     const int parts = (k_bytes + ROW - 1) / ROW;
     Step f[2];
-    load(x, w, s0, 0);
-    load(x, w, s1, 1);
-    if (STAGES == 3) load(x, w, s2, 2);
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) load(x, w, stage[i], i / GROUPS, i % GROUPS);
     wait_loads<(STAGES - 1) * kLoads>();
     meet();
-    read(f[0], s0, 0);
-    int p = 0;
-    const char *last = s0;
-    if (STAGES == 3) {
-      for (; p + 3 < parts; p += 3) {
-        part<0>(p, x, w, s0, s1, f, acc, used);
-        part<0>(p + 1, x, w, s1, s2, f, acc, used);
-        part<0>(p + 2, x, w, s2, s0, f, acc, used);
-      }
-      if (p + 1 < parts) part<0>(p, x, w, s0, s1, f, acc, used);
-      if (p + 2 < parts) part<0>(p + 1, x, w, s1, s2, f, acc, used);
-      last = p + 1 == parts ? s0 : p + 2 == parts ? s1 : s2;
-    } else {
-      for (; p + 2 < parts; p += 2) {
-        part<0>(p, x, w, s0, s1, f, acc, used);
-        part<kFlip>(p + 1, x, w, s1, s0, f, acc, used);
-      }
-      if (p + 1 < parts) {
-        part<0>(p, x, w, s0, s1, f, acc, used);
-        if (kFlip) f[0] = f[1];
-        last = s1;
-      }
-    }
-    if (used) {
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        if (s + 1 < kSteps) read(f[(s + 1) & 1], last, s + 1);
-        multiply_last(f[s & 1], s, k_bytes - (parts - 1) * ROW, acc);
-      }
-    }
+    read(f[0], stage[0], 0);
+    int k = 0;
+    for (; k + kStep < parts; k += kStep) turn<0, false>(k, parts, k_bytes, x, w, stage, f, acc, used);
+    for (; k < parts; k += kStep) turn<0, true>(k, parts, k_bytes, x, w, stage, f, acc, used);
     wait_loads<0>();
     meet();
   }
-  // row_of(r): start of row r of the tile; a row behind the end may be any other one
+
+  // The same by way of registers, for rows whose chunks are no multiples of 16 bytes in memory (a 16-byte load may start anywhere) or end
+  // inside one; what is behind the end of a row is zero.  row_of(r): start of row r of the first group's parts; a row behind the
+  // end may be any other one.  rows_w: rows of w from the first group's first one on.
+  static __device__ __forceinline__ void fetch(i32x4 (&reg)[kLoads], const char *const (&from)[kLoads], int k, int h, int64_t group, int rows_w, int k_bytes) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const bool there = GROUPS == 1 || piece_of_x(i) || piece_row(i) - BM + h * BN < rows_w;
+      const char *p = from[i] + (GROUPS > 1 && !piece_of_x(i) && there ? h * group : 0);
+      reg[i] = chunk_of<E>(p, k * ROW + piece_chunk(i) * 16, there ? k_bytes : 0);
+    }
+  }
+  static __device__ __forceinline__ void put(char *stage, const i32x4 (&reg)[kLoads]) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<i32x4 *>(stage + piece(i) * 1024 + (threadIdx.x & 63) * 16) = reg[i];
+  }
   template <class RowOf>
-  static __device__ __forceinline__ void product_staged(RowOf row_of, char *s0, char *s1, int k_bytes, f32x16 (&acc)[kTN][kTM], bool used = true) {
+  static __device__ __forceinline__ void product_staged(RowOf row_of, int64_t group, int rows_w, char *s0, char *s1, int k_bytes, Sums &acc,
+                                                        unsigned used = ~0u) {
+    constexpr int kTwo = GROUPS % 2 == 0 ? GROUPS : 2 * GROUPS;                 // parts in a turn of two stages
     const int parts = (k_bytes + ROW - 1) / ROW;
     const char *from[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) from[i] = row_of(piece_row(i));
-    i32x4 ahead[2][kLoads];                            // parts on their way: p + 1, p + 2
-    fetch(ahead[0], from, 0, k_bytes);
-    fetch(ahead[1], from, 1, k_bytes);
+    i32x4 ahead[2][kLoads];                            // the next two parts, on their way
+    fetch(ahead[0], from, 0, 0, group, rows_w, k_bytes);
+    fetch(ahead[1], from, 1 / GROUPS, 1 % GROUPS, group, rows_w, k_bytes);
     put(s0, ahead[0]);
     meet();
-    for (int p = 0; p < parts; p += 2) {
+    for (int k = 0; k < parts; k += kTwo / GROUPS) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const char *here = i ? s1 : s0;
-        if (p + i >= parts) break;
-        fetch(ahead[i], from, p + i + 2, k_bytes);
+      for (int i = 0; i < kTwo; ++i) {
+        if (k + i / GROUPS >= parts) break;
+        fetch(ahead[i & 1], from, k + (i + 2) / GROUPS, (i + 2) % GROUPS, group, rows_w, k_bytes);
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
           Step f;
-          read(f, here, s);
-          if (used) multiply(f, acc);
+          read(f, i & 1 ? s1 : s0, s);
+          if (GROUPS == 1 || (used >> (i % GROUPS) & 1)) multiply(f, acc[i % GROUPS]);
         }
-        put(i ? s0 : s1, ahead[1 - i]);                // nobody reads there since the waves last met
+        put(i & 1 ? s0 : s1, ahead[1 - (i & 1)]);      // nobody reads there since the waves last met
         meet();
       }
     }
@@ -359,22 +353,20 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_kernel(L
   const int n0 = (int)(tile % a.tiles_n) * BN;
   const char *x = static_cast<const char *>(a.x), *w = static_cast<const char *>(a.w);
   constexpr int kSize = (int)sizeof(typename E::T);
-  f32x16 acc[T::kTN][T::kTM];
-#pragma unroll
-  for (int i = 0; i < T::kTN; ++i)
-#pragma unroll
-    for (int j = 0; j < T::kTM; ++j) acc[i][j] = f32x16{};
+  typename T::Sums sums = {};
+  f32x16 (&acc)[T::kTN][T::kTM] = sums[0];
   const char *xt = x + m0 * a.x_stride * kSize, *wt = w + (int64_t)n0 * a.w_stride * kSize;   // the tile's first rows
   if (DIRECT) {
     T t;
-    t.aim([&](int r) { return r < BM ? r * (int)a.x_stride * kSize : (r - BM) * (int)a.w_stride * kSize; });
-    t.product(buffer(xt, bytes_behind(a.rows - m0, a.x_stride, a.k, kSize)), buffer(wt, bytes_behind(a.n - n0, a.w_stride, a.k, kSize)), s0, s1, s2,
-              a.k * kSize, acc);
+    t.aim([&](int r) { return r < BM ? r * (int)a.x_stride * kSize : (r - BM) * (int)a.w_stride * kSize; }, 0);
+    char *const stage[3] = {s0, s1, s2};
+    t.product(buffer(xt, bytes_behind(a.rows - m0, a.x_stride, a.k, kSize)), buffer(wt, bytes_behind(a.n - n0, a.w_stride, a.k, kSize)), stage,
+              a.k * kSize, sums);
   } else {
     T::product_staged([&](int r) {
       const int64_t m = m0 + r < a.rows ? r : a.rows - 1 - m0, n = n0 + (r - BM) < a.n ? r - BM : a.n - 1 - n0;
       return r < BM ? xt + m * a.x_stride * kSize : wt + n * a.w_stride * kSize;
-    }, s0, s1, a.k * kSize, acc);
+    }, 0, 0, s0, s1, a.k * kSize, sums);
   }
 
   // Epilogue: 32 rows at a time go through the wave's own part of LDS, so that a lane gets 8 neighbouring columns of a row.
@@ -477,41 +469,40 @@ struct LoglikesArgs {
   int32_t seqs, frames, k, v, bias_dtype, out_dtype;
 };
 
-// one or two neighbouring results
-__device__ __forceinline__ void store2(void *p, int64_t i, int dtype, bool both, float v0, float v1) {
-  if (!both) { store_as(p, i, dtype, v0); return; }
-  if (dtype == 0) {
-    typedef float pair __attribute__((ext_vector_type(2), aligned(4)));
-    *reinterpret_cast<pair *>(static_cast<float *>(p) + i) = pair{v0, v1};
+// 4 neighbouring results, or the first `count` of them
+__device__ __forceinline__ void store4(void *p, int64_t i, int dtype, int count, const float (&v)[4]) {
+  if (count < 4) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < count) store_as(p, i + e, dtype, v[e]);
+  } else if (dtype == 0) {
+    *reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + i) = f32x4{v[0], v[1], v[2], v[3]};
   } else if (dtype == 1) {
-    typedef _Float16 pair __attribute__((ext_vector_type(2), aligned(2)));
-    *reinterpret_cast<pair *>(static_cast<_Float16 *>(p) + i) = pair{(_Float16)v0, (_Float16)v1};
+    typedef _Float16 four __attribute__((ext_vector_type(4), aligned(2)));
+    *reinterpret_cast<four *>(static_cast<_Float16 *>(p) + i) = four{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
   } else {
-    typedef __bf16 pair __attribute__((ext_vector_type(2), aligned(2)));
-    *reinterpret_cast<pair *>(static_cast<__bf16 *>(p) + i) = pair{(__bf16)v0, (__bf16)v1};
+    typedef __bf16 four __attribute__((ext_vector_type(4), aligned(2)));
+    *reinterpret_cast<four *>(static_cast<__bf16 *>(p) + i) = four{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
   }
 }
 
-// The product with log-softmax behind it: a workgroup has BM whole rows, and a wave WM x WN of the sums.  A lane has 16 sums of one row
-// per 32 classes: the row's maximum and sum are the lane's own, then its neighbour's across the half wave, then, if waves lie side
-// by side (kWavesN > 1), theirs through LDS.  The log-probabilities leave through LDS too, rows at a time and in the order of memory.
-template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES, bool DIRECT>
-__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void loglikes_kernel(LoglikesArgs a) {
-  using T = Tile<E, BM, BN, WM, WN, ROW, STAGES>;
+// The product with log-softmax behind it: a workgroup has BM whole rows, GROUPS * BN classes wide.  A lane has 16 sums of one row per 32
+// classes: the row's maximum and sum are the lane's own, then its neighbour's across the half wave, then, if waves lie side
+// by side (kWavesN > 1), theirs through LDS.  The log-probabilities leave from the registers, 4 neighbours at a time: a wave's
+// stores together fill whole lines of the L2.
+// Tiles differ with the number of classes and of frames; what a frame gets does not: k goes by 16 elements at a time in every one of
+// them, and a row's sum is that of its 32 classes at a time, in their order.
+template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES, int GROUPS, bool DIRECT, int PER_SIMD>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), PER_SIMD) void loglikes_kernel(LoglikesArgs a) {
+  using T = Tile<E, BM, BN, WM, WN, ROW, STAGES, GROUPS>;
   constexpr int kSize = (int)sizeof(typename E::T);
-  // Rows of results that LDS takes at a time: of each wave (two waves' in a stage), or of the workgroup (in all stages).
   constexpr bool kAlone = T::kWavesN == 1;
-  constexpr int kRowsOut = kAlone ? (BN <= 64 ? 32 : BN <= 160 ? 16 : 8) : (T::kStage / (BN * 4) >= 16 ? 16 : 8);
-  constexpr int kLds = kAlone && 2 * kRowsOut * BN * 4 > T::kStage ? 2 * kRowsOut * BN * 4 : T::kStage;
-  static_assert(kAlone ? T::kWaves <= 4 : BM == WM && kRowsOut * BN * 4 <= T::kStage, "the results fit the stages; a wave has whole rows or a part of each");
-  __shared__ __align__(16) char s0[kLds], s1[kLds], s2[STAGES == 3 ? kLds : 16];
-  __shared__ float row_part[kAlone ? 1 : T::kWavesN][BM];
-  __shared__ __align__(16) float bias[BN], prior[BN];
+  __shared__ __align__(16) char s0[T::kStage], s1[T::kStage], s2[STAGES > 2 ? T::kStage : 16], s3[STAGES > 3 ? T::kStage : 16];
+  __shared__ float row_part[kAlone ? 1 : GROUPS * BN / 32][BM];       // of 32 classes each
+  constexpr int kClasses = GROUPS * BN, kMine = (kClasses + T::kThreads - 1) / T::kThreads;
+  static_assert(kClasses * 8 <= T::kStage, "bias and priors fit a stage");
+  float *bias = reinterpret_cast<float *>(s0), *prior = bias + kClasses;      // (there behind the product)
   const unsigned rows = (unsigned)a.seqs * a.frames, m0 = blockIdx.x * BM, frames = a.frames;      // (at most 2^31 - 1 rows)
-  for (int c = threadIdx.x; c < BN; c += T::kThreads) {
-    bias[c] = a.bias && c < a.v ? load_as(a.bias, c, a.bias_dtype) : 0.0f;
-    prior[c] = a.log_prior && c < a.v ? a.log_prior[c] : 0.0f;
-  }
   // is there a frame before its sequence's length among them?
   bool any = false;
   for (int r = threadIdx.x; r < BM && m0 + r < rows; r += T::kThreads)
@@ -530,42 +521,68 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void loglikes_kernel
   auto w_offset = [&](int r) { return (int64_t)(r - BM < a.v ? r - BM : a.v - 1) * a.w_stride * kSize; };
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave / T::kWavesN, wn = wave % T::kWavesN;
-  const bool used = kAlone || wn * WN < a.v;          // waves whose classes are all behind v only load and store
-  f32x16 acc[T::kTN][T::kTM];
+  unsigned used = 0;                                   // groups in which this wave has classes before v
 #pragma unroll
-  for (int i = 0; i < T::kTN; ++i)
+  for (int h = 0; h < GROUPS; ++h) used |= h * BN + wn * WN < a.v ? 1u << h : 0;
+  used = __builtin_amdgcn_readfirstlane(used);
+  float my_bias[kMine], my_prior[kMine];               // on their way while the product is taken
 #pragma unroll
-    for (int j = 0; j < T::kTM; ++j) acc[i][j] = f32x16{};
+  for (int i = 0; i < kMine; ++i) {
+    const int c = threadIdx.x + i * T::kThreads;
+    my_bias[i] = a.bias && c < a.v ? load_as(a.bias, c, a.bias_dtype) : 0.0f;
+    my_prior[i] = a.log_prior && c < a.v ? a.log_prior[c] : 0.0f;
+  }
+  typename T::Sums acc = {};
   if (DIRECT) {
     T t;
-    t.aim([&](int r) { return r < BM ? (int)x_offset(r) : r - BM < a.v ? (int)w_offset(r) : 0x7fffff00; });      // (out of bounds: not read)
+    t.aim([&](int r) { return (int)(r < BM ? x_offset(r) : w_offset(r)); }, BN * (int)a.w_stride * kSize);
     const int64_t x_end = (int64_t)(a.seqs - 1) * a.x_seq_stride + (int64_t)(a.frames - 1) * a.x_stride + a.k;      // (within 2 GB here)
-    t.product(buffer(x, (uint32_t)(x_end * kSize)), buffer(w, bytes_behind(a.v, a.w_stride, a.k, kSize)), s0, s1, s2, a.k * kSize, acc, used);
+    char *const all[4] = {s0, s1, s2, s3};
+    char *stage[STAGES];
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) stage[i] = all[i];
+    t.product(buffer(x, (uint32_t)(x_end * kSize)), buffer(w, bytes_behind(a.v, a.w_stride, a.k, kSize)), stage, a.k * kSize, acc, used);
   } else {
-    T::product_staged([&](int r) { return r < BM ? x + x_offset(r) : w + w_offset(r); }, s0, s1, a.k * kSize, acc, used);
+    T::product_staged([&](int r) { return r < BM ? x + x_offset(r) : w + w_offset(r); }, BN * a.w_stride * kSize, a.v, s0, s1, a.k * kSize, acc, used);
   }
 
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int c = threadIdx.x + i * T::kThreads;
+    if (c < kClasses) { bias[c] = my_bias[i]; prior[c] = my_prior[i]; }
+  }
+  __syncthreads();
   // sums -> z = sum + bias; classes behind v count as -inf
-#pragma unroll
-  for (int i = 0; i < T::kTN; ++i)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int c = wn * WN + 32 * i + 8 * q + 4 * (lane >> 5);
-      const f32x4 b = *reinterpret_cast<const f32x4 *>(bias + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int j = 0; j < T::kTM; ++j) acc[i][j][4 * q + e] = c + e < a.v ? acc[i][j][4 * q + e] + b[e] : -__builtin_inff();
-    }
-  // the rows' maxima
   float m[T::kTM], ls[T::kTM];
 #pragma unroll
+  for (int j = 0; j < T::kTM; ++j) m[j] = -__builtin_inff();
+#pragma unroll
+  for (int h = 0; h < GROUPS; ++h)
+#pragma unroll
+    for (int i = 0; i < T::kTN; ++i) {
+      const int c0 = h * BN + wn * WN + 32 * i + 4 * (lane >> 5);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 b = *reinterpret_cast<const f32x4 *>(bias + c0 + 8 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int j = 0; j < T::kTM; ++j) acc[h][i][j][4 * q + e] += b[e];
+      }
+      if (h * BN + wn * WN + 32 * i + 32 > a.v) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+#pragma unroll
+          for (int j = 0; j < T::kTM; ++j) acc[h][i][j][q] = c0 + 8 * (q / 4) + q % 4 < a.v ? acc[h][i][j][q] : -__builtin_inff();
+      }
+#pragma unroll
+      for (int j = 0; j < T::kTM; ++j)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) m[j] = fmaxf(m[j], acc[h][i][j][q]);
+    }
+  // the rows' maxima
+#pragma unroll
   for (int j = 0; j < T::kTM; ++j) {
-    m[j] = -__builtin_inff();
-#pragma unroll
-    for (int i = 0; i < T::kTN; ++i)
-#pragma unroll
-      for (int q = 0; q < 16; ++q) m[j] = fmaxf(m[j], acc[i][j][q]);
     m[j] = fmaxf(m[j], __shfl_xor(m[j], 32));
     if (!kAlone && lane < 32) row_part[wn][wm * WM + 32 * j + lane] = m[j];
   }
@@ -582,99 +599,55 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void loglikes_kernel
   for (int j = 0; j < T::kTM; ++j) {
     ls[j] = 0.0f;
 #pragma unroll
-    for (int i = 0; i < T::kTN; ++i) {
-      float part = 0.0f;
+    for (int h = 0; h < GROUPS; ++h)
 #pragma unroll
-      for (int q = 0; q < 16; ++q) part += exp_fast(acc[i][j][q] - m[j]);
-      ls[j] += part;
-    }
-    ls[j] += __shfl_xor(ls[j], 32);
-    if (!kAlone && lane < 32) row_part[wn][wm * WM + 32 * j + lane] = ls[j];
+      for (int i = 0; i < T::kTN; ++i) {
+        float part = 0.0f;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          acc[h][i][j][q] -= m[j];
+          part += exp_fast(acc[h][i][j][q]);
+        }
+        part += __shfl_xor(part, 32);
+        ls[j] += part;
+        if (!kAlone && lane < 32) row_part[h * (BN / 32) + wn * T::kTN + i][wm * WM + 32 * j + lane] = part;
+      }
   }
   if (!kAlone) {
     __syncthreads();
+    const int parts = (a.v - 1) / 32 + 1;
 #pragma unroll
-    for (int j = 0; j < T::kTM; ++j) {
-      ls[j] = 0.0f;
+    for (int j = 0; j < T::kTM; ++j) ls[j] = 0.0f;
+#pragma unroll 8
+    for (int n = 0; n < parts; ++n)
 #pragma unroll
-      for (int n = 0; n < T::kWavesN; ++n) ls[j] += row_part[n][wm * WM + 32 * j + (lane & 31)];
-    }
+      for (int j = 0; j < T::kTM; ++j) ls[j] += row_part[n][wm * WM + 32 * j + (lane & 31)];
   }
 #pragma unroll
   for (int j = 0; j < T::kTM; ++j) {
-    ls[j] = logf(ls[j]);
+    const float log_sum = logf(ls[j]);
+    const unsigned row = m0 + wm * WM + 32 * j + (lane & 31);
+    const int s = (int)(row / frames), t = (int)(row % frames);
+    if (row >= rows || (a.lengths && t >= a.lengths[s])) continue;
+    const int64_t to = s * a.out_seq_stride + t * a.out_stride;
 #pragma unroll
-    for (int i = 0; i < T::kTN; ++i)
+    for (int h = 0; h < GROUPS; ++h)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x4 off = *reinterpret_cast<const f32x4 *>(prior + wn * WN + 32 * i + 8 * q + 4 * (lane >> 5));
+      for (int i = 0; i < T::kTN; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = ((acc[i][j][4 * q + e] - m[j]) - ls[j]) - off[e];
-      }
-  }
-
-  // rows r0.. of the results into `to`, a.v floats each: the lanes that have them write
-  auto leave = [&](float *to, int j, int r0, int n) {
-    const int r = (lane & 31) - r0;
-    if (r < 0 || r >= n) return;
+        for (int q = 0; q < 4; ++q) {
+          const int c = h * BN + wn * WN + 32 * i + 8 * q + 4 * (lane >> 5);
+          if (c >= a.v) continue;
+          float l[4];
 #pragma unroll
-    for (int i = 0; i < T::kTN; ++i)
+          for (int e = 0; e < 4; ++e) l[e] = acc[h][i][j][4 * q + e] - log_sum;
+          if (a.log_prior) {
+            const f32x4 off = *reinterpret_cast<const f32x4 *>(prior + c);
 #pragma unroll
-      for (int q = 0; q < 16; ++q) {
-        const int c = wn * WN + 32 * i + 8 * (q / 4) + 4 * (lane >> 5) + q % 4;
-        if (c < a.v) to[r * a.v + c] = acc[i][j][q];
-      }
-  };
-  if constexpr (kAlone) {
-    float *out = reinterpret_cast<float *>((wave < 2 ? s0 : s1) + (wave & 1) * (kRowsOut * BN * 4));
-#pragma unroll
-    for (int j = 0; j < T::kTM; ++j)
-      for (int r0 = 0; r0 < 32; r0 += kRowsOut) {
-        leave(out, j, r0, kRowsOut);
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        const unsigned first = m0 + wm * WM + 32 * j + r0;
-        int s = (int)(first / frames), t = (int)(first % frames);
-        // a sequence's frames among them at a time: contiguous results go out as one run
-        for (int r = 0; r < kRowsOut && s < a.seqs; ++s, t = 0) {
-          const int here = kRowsOut - r < a.frames - t ? kRowsOut - r : a.frames - t;
-          const int length = a.lengths ? a.lengths[s] : a.frames;
-          const int n = length <= t ? 0 : length - t < here ? length - t : here;
-          if (n > 0 && a.out_stride == a.v) {
-            const int64_t to = s * a.out_seq_stride + t * a.out_stride;
-            for (int c = 2 * lane; c < n * a.v; c += 128)
-              store2(a.out, to + c, a.out_dtype, c + 1 < n * a.v, out[r * a.v + c], out[r * a.v + c + 1]);
-          } else {
-            for (int i = 0; i < n; ++i)
-              for (int c = 2 * lane; c < a.v; c += 128)
-                store2(a.out, s * a.out_seq_stride + (t + i) * a.out_stride + c, a.out_dtype, c + 1 < a.v, out[(r + i) * a.v + c], out[(r + i) * a.v + c + 1]);
+            for (int e = 0; e < 4; ++e) l[e] -= off[e];
           }
-          r += here;
+          store4(a.out, to + c, a.out_dtype, a.v - c, l);
         }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      }
-  } else {
-    // kRowsOut rows in each stage (of which two are used, so that the same code does for two and three)
-#pragma unroll
-    for (int j = 0; j < T::kTM; ++j)
-      for (int r0 = 0; r0 < 32; r0 += 2 * kRowsOut) {
-        leave(reinterpret_cast<float *>(s0), j, r0, kRowsOut);
-        leave(reinterpret_cast<float *>(s1), j, r0 + kRowsOut, kRowsOut);
-        __syncthreads();
-        for (int r = wave; r < 2 * kRowsOut; r += T::kWaves) {
-          const unsigned row = m0 + 32 * j + r0 + r;
-          if (row >= rows) break;
-          const int s = (int)(row / frames), t = (int)(row % frames);
-          if (a.lengths && t >= a.lengths[s]) continue;
-          const float *from = reinterpret_cast<const float *>(r < kRowsOut ? s0 : s1) + (r % kRowsOut) * a.v;
-          for (int c = 2 * lane; c < a.v; c += 128)
-            store2(a.out, s * a.out_seq_stride + t * a.out_stride + c, a.out_dtype, c + 1 < a.v, from[c], from[c + 1]);
-        }
-        __syncthreads();
-      }
   }
 }
 

@@ -101,22 +101,36 @@ template <class E> int run_linear(LinearArgs a, bool direct, void *stream) {
   return direct ? run_tiles<E, 64, 64, 32, 32, 128, true>(a, stream) : run_tiles<E, 64, 64, 32, 32, 128, false>(a, stream);
 }
 
-template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES>
+template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES, int GROUPS, int PER_SIMD>
 int run_rows(const LoglikesArgs &a, bool direct, void *stream) {
   const int64_t blocks = ((int64_t)a.seqs * a.frames - 1) / BM + 1;
   constexpr int kThreads = 64 * (BM / WM) * (BN / WN);
-  return direct ? launch("wfst_loglikes", loglikes_kernel<E, BM, BN, WM, WN, ROW, STAGES, true>, blocks, kThreads, a, stream)
-                : launch("wfst_loglikes", loglikes_kernel<E, BM, BN, WM, WN, ROW, STAGES, false>, blocks, kThreads, a, stream);
+  return direct ? launch("wfst_loglikes", loglikes_kernel<E, BM, BN, WM, WN, ROW, STAGES, GROUPS, true, PER_SIMD>, blocks, kThreads, a, stream)
+                : launch("wfst_loglikes", loglikes_kernel<E, BM, BN, WM, WN, ROW, STAGES, GROUPS, false, PER_SIMD>, blocks, kThreads, a, stream);
 }
 
-// The narrowest tile that has a whole row.  Up to 256 classes a wave has 32 rows of its own; behind that the waves lie side by side.
+// The narrowest tile that has a whole row, 32 rows high for few frames, when a frame's time is a chain of parts of k, and else as high as
+// registers allow, since w is read once per tile.  Up to 256 classes the waves of a high tile have 32 rows each; else they lie
+// side by side.  us at k 512, 16 bits, low / high tiles, 129 classes: 16 frames 7.0 / 11.7, 4,096: 7.7 / 13.1, 16,384: 11.4 / 15.9,
+// 118,000: 115 / 66; 256 classes: 8.5 / 17, 9.9 / 18, 19 / 21, 197 / 86; 500: 12 / 14, 15 / 17, 35 / 27; 1,000: 20 / 24, 24 / 29, 62 / 45.
 template <class E> int run_loglikes(const LoglikesArgs &a, bool direct, void *stream) {
-  if (a.v <= 64) return run_rows<E, 128, 64, 32, 64, 64, 3>(a, direct, stream);
-  if (a.v <= 160) return run_rows<E, 128, 160, 32, 160, 64, 3>(a, direct, stream);
-  if (a.v <= 256) return run_rows<E, 128, 256, 32, 256, 64, 3>(a, direct, stream);
-  if (a.v <= 512) return run_rows<E, 64, 512, 64, 64, 64, 3>(a, direct, stream);
-  if (a.v <= 1024) return run_rows<E, 64, 1024, 64, 64, 64, 2>(a, direct, stream);
-  return run_rows<E, 32, 2048, 32, 128, 32, 2>(a, direct, stream);
+  const int64_t rows = (int64_t)a.seqs * a.frames;
+  if (rows <= 8192) {
+    if (a.v <= 64) return run_rows<E, 32, 64, 32, 32, 128, 4, 1, 1>(a, direct, stream);
+    if (a.v <= 160) return run_rows<E, 32, 160, 32, 32, 64, 4, 1, 2>(a, direct, stream);
+    if (a.v <= 256) return run_rows<E, 32, 256, 32, 32, 128, 4, 1, 2>(a, direct, stream);
+  }
+  if (rows <= 4096) {
+    if (a.v <= 512) return run_rows<E, 32, 512, 32, 32, 64, 4, 1, 4>(a, direct, stream);
+    if (a.v <= 1024) return run_rows<E, 32, 512, 32, 32, 64, 4, 2, 4>(a, direct, stream);
+  }
+  if (a.v <= 64) return run_rows<E, 128, 64, 32, 64, 64, 2, 1, 4>(a, direct, stream);
+  if (a.v <= 160) return run_rows<E, 128, 160, 32, 160, 64, 2, 1, 3>(a, direct, stream);
+  if (a.v <= 256) return run_rows<E, 128, 256, 32, 256, 64, 2, 1, 2>(a, direct, stream);
+  if (a.v <= 512) return run_rows<E, 64, 512, 64, 64, 64, 2, 1, 4>(a, direct, stream);
+  if (a.v <= 1024) return run_rows<E, 64, 512, 64, 64, 64, 4, 2, 2>(a, direct, stream);
+  if (a.v <= 1152) return run_rows<E, 64, 384, 64, 32, 64, 4, 3, 3>(a, direct, stream);
+  return run_rows<E, 32, 512, 32, 64, 64, 4, 4, 2>(a, direct, stream);
 }
 
 // Long rows are cut until there are about 1,024 workgroups, into parts of 8,192 scores at least and 64 of them at most.
@@ -176,6 +190,7 @@ int32_t wfst_linear(const wfst_linear_args *args, void *stream) {
   if (!aligned(p.x, size) || !aligned(p.w, size) || !aligned(p.y, out_size) || !aligned(p.residual, out_size) ||
       (p.bias && !aligned(p.bias, type_size(p.bias_dtype))))
     return refuse(me, "an address is not a multiple of its element's size");
+  if (p.k > 1 << 28) return refuse(me, "k must be at most 2^28");
   const int64_t nx = span(1, p.rows, p.k, 0, p.x_stride, size), nw = span(1, p.n, p.k, 0, p.w_stride, size);
   const int64_t ny = span(1, p.rows, p.n, 0, p.y_stride, out_size), nr = p.residual ? span(1, p.rows, p.n, 0, p.residual_stride, out_size) : 0;
   if (nx < 0 || nw < 0 || ny < 0 || nr < 0) return refuse(me, "sizes and strides are too large");
@@ -204,6 +219,7 @@ int32_t wfst_loglikes(const wfst_loglikes_args *args, void *stream) {
   if (!aligned(p.x, size) || !aligned(p.w, size) || !aligned(p.out, out_size) || !aligned(p.log_prior, 4) || !aligned(p.lengths, 4) ||
       (p.bias && !aligned(p.bias, type_size(p.bias_dtype))))
     return refuse(me, "an address is not a multiple of its element's size");
+  if (p.k > 1 << 28) return refuse(me, "k must be at most 2^28");
   if ((int64_t)p.seqs * p.frames > INT_MAX) return refuse(me, "more than 2^31 - 1 frames");
   const int64_t nx = span(p.seqs, p.frames, p.k, p.x_seq_stride, p.x_stride, size), nw = span(1, p.v, p.k, 0, p.w_stride, size);
   const int64_t no = span(p.seqs, p.frames, p.v, p.out_seq_stride, p.out_stride, out_size);

@@ -210,7 +210,7 @@ def check_loglikes(x, w, b=None, prior=None, lengths=None, out=None, out_dtype=N
 @pytest.mark.parametrize("v", [1, 2, 29, 32, 33, 64, 100, 129, 160, 161, 256, 257, 500, 512, 513, 1024, 1025, 2047, 2048])
 def test_loglikes(v, dt):
     g = gen(v)
-    for rows, k in ((1, 64), (16, 512), (37, 88), (150, 65), (270, 256)):
+    for rows, k in ((1, 64), (16, 512), (37, 88), (150, 65), (270, 256), (8200, 72), (8193, 35)):
         x, w = randn(g, rows, k).to(DT[dt]), (randn(g, v, k) * 2 / math.sqrt(k)).to(DT[dt])
         b = randn(g, v) if rows % 2 else randn(g, v).to(DT[dt])
         check_loglikes(x, w, b, torch.log_softmax(randn(g, v), 0) if rows > 20 else None, out_dtype=DT[dt] if rows % 3 else torch.float32)
@@ -261,6 +261,20 @@ def test_loglikes_strides(dt):
     one = randn(g, k).to(DT[dt])
     got = loglikes(one.expand(B, T, k), w, b)                                      # the same frame everywhere
     assert torch.equal(got, got[:1, :1].expand(B, T, v))
+
+
+@pytest.mark.parametrize("v", [29, 129, 200, 500, 1000, 1100, 2048])
+def test_a_frame_gets_the_same_bits_in_any_company(v):
+    """Alone, in a chunk, in a batch of any size (other tiles): so chunks decode as the whole utterance does."""
+    g = gen(v, 6)
+    for dt, k in ((torch.bfloat16, 128), (torch.float32, 33), (torch.float16, 36)):
+        x, w, b = randn(g, 8300, k).to(dt), (randn(g, v, k) / 8).to(dt), randn(g, v)
+        whole = loglikes(x, w, b)
+        for n in (1, 16, 33, 4097):
+            assert torch.equal(loglikes(x[:n], w, b), whole[:n])
+        lengths = torch.tensor([8200, 0, 100], dtype=torch.int32, device="cuda")
+        got = loglikes(x.expand(3, 8300, k), w, b, lengths=lengths)
+        assert torch.equal(got[0, :8200], whole[:8200]) and torch.equal(got[2, :100], whole[:100])
 
 
 @pytest.mark.parametrize("v", [29, 129, 700])
