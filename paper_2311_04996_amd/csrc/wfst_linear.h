@@ -498,28 +498,65 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), PER_SIMD) void loglikes
   constexpr int kSize = (int)sizeof(typename E::T);
   constexpr bool kAlone = T::kWavesN == 1;
   __shared__ __align__(16) char s0[T::kStage], s1[T::kStage], s2[STAGES > 2 ? T::kStage : 16], s3[STAGES > 3 ? T::kStage : 16];
+  __shared__ int64_t x_at[BM], out_at[BM];             // where a row's frame is, in bytes behind x, and its results (-1: nowhere)
   __shared__ float row_part[kAlone ? 1 : GROUPS * BN / 32][BM];       // of 32 classes each
   constexpr int kClasses = GROUPS * BN, kMine = (kClasses + T::kThreads - 1) / T::kThreads;
-  static_assert(kClasses * 8 <= T::kStage, "bias and priors fit a stage");
+  constexpr int kPacked = 1024;
+  static_assert(kClasses * 8 <= T::kStage && (kPacked + 1) * 4 <= T::kStage, "what a stage holds before and behind the product fits");
   float *bias = reinterpret_cast<float *>(s0), *prior = bias + kClasses;      // (there behind the product)
   const unsigned rows = (unsigned)a.seqs * a.frames, m0 = blockIdx.x * BM, frames = a.frames;      // (at most 2^31 - 1 rows)
-  // is there a frame before its sequence's length among them?
-  bool any = false;
-  for (int r = threadIdx.x; r < BM && m0 + r < rows; r += T::kThreads)
-    any |= !a.lengths || (int)((m0 + r) % frames) < a.lengths[(m0 + r) / frames];
-  if (!__syncthreads_or(any)) return;
-  const char *x = static_cast<const char *>(a.x), *w = static_cast<const char *>(a.w);
-  // Row r of x in the tile, in bytes behind x.  A frame behind the length is not read: the sequence's last one before it (or its
-  // first one) stands in.
-  auto x_offset = [&](int r) {
-    const unsigned m = m0 + r < rows ? m0 + r : rows - 1;
-    const int s = (int)(m / frames);
-    int t = (int)(m % frames);
-    if (a.lengths && t >= a.lengths[s]) t = a.lengths[s] > 0 ? a.lengths[s] - 1 : 0;
-    return (s * a.x_seq_stride + t * a.x_stride) * kSize;
-  };
-  auto w_offset = [&](int r) { return (int64_t)(r - BM < a.v ? r - BM : a.v - 1) * a.w_stride * kSize; };
+  // The frames of the tile.  With lengths they are taken from those before them only, one sequence's behind the other's, so that no
+  // tile has padding in it (more than kPacked sequences: padding stays among them, and is not written).
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (a.lengths && a.seqs <= kPacked) {
+    int *start = reinterpret_cast<int *>(s0);          // of a sequence's frames among all
+    for (int i = threadIdx.x; i < a.seqs; i += T::kThreads) {
+      const int n = a.lengths[i];
+      start[i + 1] = n < 0 ? 0 : n < a.frames ? n : a.frames;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      const int each = (a.seqs + 63) / 64, from = lane * each, to = from + each < a.seqs ? from + each : a.seqs;
+      int sum = 0;
+      for (int i = from; i < to; ++i) sum += start[i + 1];
+      int before = sum;
+      for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(before, d);
+        before += lane >= d ? o : 0;
+      }
+      before -= sum;
+      for (int i = from; i < to; ++i) start[i + 1] = before += start[i + 1];
+      if (lane == 0) start[0] = 0;
+    }
+    __syncthreads();
+    const unsigned total = start[a.seqs];
+    if (m0 >= total) return;
+    for (int r = threadIdx.x; r < BM; r += T::kThreads) {
+      const unsigned i = m0 + r < total ? m0 + r : total - 1;
+      int s = 0;                                       // the last sequence that starts at i or before it
+      for (int d = kPacked; d; d >>= 1)
+        if (s + d < a.seqs && (unsigned)start[s + d] <= i) s += d;
+      const int t = (int)i - start[s];
+      x_at[r] = (s * a.x_seq_stride + t * a.x_stride) * kSize;
+      out_at[r] = m0 + r < total ? s * a.out_seq_stride + t * a.out_stride : -1;
+    }
+  } else {
+    bool any = false;
+    for (int r = threadIdx.x; r < BM; r += T::kThreads) {
+      const unsigned i = m0 + r < rows ? m0 + r : rows - 1;
+      const int s = (int)(i / frames), n = a.lengths ? a.lengths[s] : a.frames;
+      int t = (int)(i % frames);
+      const bool there = m0 + r < rows && t < n;
+      out_at[r] = there ? s * a.out_seq_stride + t * a.out_stride : -1;
+      if (t >= n) t = n > 0 ? n - 1 : 0;               // (not used: the sequence's last frame before the length stands in)
+      x_at[r] = (s * a.x_seq_stride + t * a.x_stride) * kSize;
+      any |= there;
+    }
+    if (!__syncthreads_or(any)) return;
+  }
+  __syncthreads();
+  const char *x = static_cast<const char *>(a.x), *w = static_cast<const char *>(a.w);
+  auto w_offset = [&](int r) { return (int64_t)(r - BM < a.v ? r - BM : a.v - 1) * a.w_stride * kSize; };
   const int wm = wave / T::kWavesN, wn = wave % T::kWavesN;
   unsigned used = 0;                                   // groups in which this wave has classes before v
 #pragma unroll
@@ -535,7 +572,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), PER_SIMD) void loglikes
   typename T::Sums acc = {};
   if (DIRECT) {
     T t;
-    t.aim([&](int r) { return (int)(r < BM ? x_offset(r) : w_offset(r)); }, BN * (int)a.w_stride * kSize);
+    t.aim([&](int r) { return (int)(r < BM ? x_at[r] : w_offset(r)); }, BN * (int)a.w_stride * kSize);
     const int64_t x_end = (int64_t)(a.seqs - 1) * a.x_seq_stride + (int64_t)(a.frames - 1) * a.x_stride + a.k;      // (within 2 GB here)
     char *const all[4] = {s0, s1, s2, s3};
     char *stage[STAGES];
@@ -543,7 +580,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), PER_SIMD) void loglikes
     for (int i = 0; i < STAGES; ++i) stage[i] = all[i];
     t.product(buffer(x, (uint32_t)(x_end * kSize)), buffer(w, bytes_behind(a.v, a.w_stride, a.k, kSize)), stage, a.k * kSize, acc, used);
   } else {
-    T::product_staged([&](int r) { return r < BM ? x + x_offset(r) : w + w_offset(r); }, BN * a.w_stride * kSize, a.v, s0, s1, a.k * kSize, acc, used);
+    T::product_staged([&](int r) { return r < BM ? x + x_at[r] : w + w_offset(r); }, BN * a.w_stride * kSize, a.v, s0, s1, a.k * kSize, acc, used);
   }
 
 #pragma unroll
@@ -626,10 +663,8 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), PER_SIMD) void loglikes
 #pragma unroll
   for (int j = 0; j < T::kTM; ++j) {
     const float log_sum = logf(ls[j]);
-    const unsigned row = m0 + wm * WM + 32 * j + (lane & 31);
-    const int s = (int)(row / frames), t = (int)(row % frames);
-    if (row >= rows || (a.lengths && t >= a.lengths[s])) continue;
-    const int64_t to = s * a.out_seq_stride + t * a.out_stride;
+    const int64_t to = out_at[wm * WM + 32 * j + (lane & 31)];
+    if (to < 0) continue;
 #pragma unroll
     for (int h = 0; h < GROUPS; ++h)
 #pragma unroll

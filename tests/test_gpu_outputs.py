@@ -240,6 +240,19 @@ def test_loglikes_of_a_padded_batch(v, dt):
     assert bool((out[1] == 5.0).all() and (out[6] == 5.0).all() and (out[2, 1:] == 5.0).all())
 
 
+@pytest.mark.parametrize("seqs", [1, 3, 64, 65, 1023, 1024, 1025, 3000])
+def test_loglikes_of_many_short_sequences(seqs):
+    g = gen(seqs, 12)
+    T, k, v = 5, 64, 129
+    x, w, b = randn(g, seqs, T, k).bfloat16(), randn(g, v, k).bfloat16(), randn(g, v)
+    whole = loglikes(x, w, b)
+    for lengths in (torch.randint(-1, T + 2, (seqs,), generator=g, device="cuda", dtype=torch.int32), torch.zeros(seqs, dtype=torch.int32, device="cuda"),
+                    torch.full((seqs,), T, dtype=torch.int32, device="cuda"), (torch.arange(seqs, device="cuda") == seqs - 1).int()):
+        valid = torch.arange(T, device="cuda")[None] < lengths[:, None]
+        got = loglikes(x, w, b, lengths=lengths, out=torch.full((seqs, T, v), 2.0, device="cuda"))
+        assert torch.equal(got[valid], whole[valid]) and bool((got[~valid] == 2.0).all())
+
+
 @pytest.mark.parametrize("dt", DT)
 def test_loglikes_strides(dt):
     g = gen(3)
