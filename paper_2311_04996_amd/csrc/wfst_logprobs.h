@@ -155,9 +155,10 @@ __global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a) {
 // ---- longer rows: a workgroup per part of a row
 //
 // A lane takes 16 bytes at a time, keeps the maximum of what it has seen, and scales its sums when that grows.  The top ones need
-// no list on the way: the k-th largest of the lanes' maxima is a bound that at least k scores reach, and what reaches it
-// lies with the lanes whose own maximum does.  Those, k of 256 unless scores are equal, are read again and what reaches the bound
-// is sorted.  Rows with too many equal scores, or a NaN, have their top ones searched one after the other instead.
+// no list on the way: the k-th largest of the lanes' maxima (of four lanes together up to k = 32) is a bound that at least k scores reach,
+// and what reaches it lies with the lanes whose own maximum does.  Those, little more than k of 256 unless scores are equal, are
+// read again and what reaches the bound is sorted.  Rows with too many equal scores, or a NaN, have their top ones searched
+// one after the other instead.
 constexpr int kLongThreads = 256, kLongLoads = 4, kFound = 1024;
 
 template <class E> struct Chunk {                       // 16 bytes of scores, from any address
@@ -222,13 +223,23 @@ __device__ __forceinline__ void finish_row(const LogprobsArgs &a, int64_t row, c
   }
 }
 
+// How many of n keys are above k (n reads in flight, not one after the other)
+__device__ __forceinline__ int place_of(unsigned long long k, const unsigned long long *keys, int n) {
+  int place = 0, f = 0;
+  for (; f + 8 <= n; f += 8)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) place += keys[f + i] > k;
+  for (; f < n; ++f) place += keys[f] > k;
+  return place;
+}
+
 template <class E>
 __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArgs a) {
   using C = Chunk<E>;
   constexpr int kWaves = kLongThreads / 64, kStep = kLongThreads * C::kN;       // elements that the workgroup loads at a time
   __shared__ Sums waves[kWaves];
-  __shared__ __align__(16) int lane_max[kLongThreads];
-  __shared__ int picked[kMaxTop], n_picked, n_found;
+  __shared__ __align__(16) int maxima[kLongThreads];
+  __shared__ int picked[kLongThreads], n_picked, n_found, bound_;
   __shared__ unsigned long long found[kFound], keys[kMaxTop], best[kWaves];
   const unsigned row = blockIdx.x / (unsigned)a.splits, split = blockIdx.x % (unsigned)a.splits;
   const unsigned s = row / (unsigned)a.frames, t = row % (unsigned)a.frames;
@@ -260,7 +271,16 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
     const float base = grow(q, fmaxf(q.m, chunk_max<E>(c)));
     add_chunk<E>(q, c, base);
   }
-  if (a.top) lane_max[tid] = mine < hi ? order_of(q.m) : kNothing;
+  const int own = mine < hi ? order_of(q.m) : kNothing;
+  const bool fours = a.top <= 32;
+  if (fours) {
+    int o = turned<0xb1>(own);                                  // of the lane beside, then of the two beside
+    o = o > own ? o : own;
+    const int p = turned<0x4e>(o);
+    if (tid % 4 == 0) maxima[tid / 4] = p > o ? p : o;
+  } else {
+    maxima[tid] = own;
+  }
   if (tid == 0) n_picked = n_found = 0;
 
   // the workgroup's sums: lanes, then waves
@@ -278,47 +298,78 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
     bool slow = q.sum != q.sum;                                 // a NaN (or +inf): maxima pass over it
     const int n = a.top < hi - lo ? a.top : hi - lo;            // (a row's last part may be shorter)
     if (!slow) {
-      // the bound: the n-th largest of the lanes' maxima (the lane breaks ties)
-      const int own = lane_max[tid];
-      int rank = 0;
-      for (int i = 0; i < kLongThreads; i += 4) {
-        const int4 o = *reinterpret_cast<const int4 *>(lane_max + i);
-        rank += (o.x > own || (o.x == own && i < tid)) + (o.y > own || (o.y == own && i + 1 < tid)) +
-                (o.z > own || (o.z == own && i + 2 < tid)) + (o.w > own || (o.w == own && i + 3 < tid));
-      }
-      if (rank == n - 1) picked[0] = own;
-      __syncthreads();
-      const int bound = picked[0];
-      __syncthreads();
-      if (own >= bound && own != kNothing) {
-        const int i = atomicAdd(&n_picked, 1);
-        if (i < kMaxTop) picked[i] = tid;
+      // the bound: the n-th largest of the maxima (the lower one breaks ties)
+      const int many = fours ? kLongThreads / 4 : kLongThreads;
+      if (tid < many) {
+        const int mine_ = maxima[tid];
+        int rank = 0;
+#pragma unroll 4
+        for (int i = 0; i < many; i += 4) {
+          const int4 o = *reinterpret_cast<const int4 *>(maxima + i);
+          rank += (o.x > mine_ || (o.x == mine_ && i < tid)) + (o.y > mine_ || (o.y == mine_ && i + 1 < tid)) +
+                  (o.z > mine_ || (o.z == mine_ && i + 2 < tid)) + (o.w > mine_ || (o.w == mine_ && i + 3 < tid));
+        }
+        if (rank == n - 1) bound_ = mine_;
       }
       __syncthreads();
-      slow = n_picked > kMaxTop;
-      if (!slow) {
-        // the picked lanes' chunks again, all threads
+      const int bound = bound_;
+      if (own >= bound && own != kNothing) picked[atomicAdd(&n_picked, 1)] = tid;
+      __syncthreads();
+      // the picked lanes' chunks again, all threads: scores of an order above `above`
+      const auto collect = [&](int above) {
         const int chunks = (hi - lo - 1) / kStep + 1;           // of a lane, at most
         for (int64_t i = tid; i < (int64_t)n_picked * chunks; i += kLongThreads) {
           const int64_t at = lo + picked[i / chunks] * C::kN + (i % chunks) * kStep;
-          for (int e = 0; e < C::kN && at + e < hi; ++e) {
-            const int o = order_of(E::get(x[at + e]));
-            if (o >= bound) {
+          typename C::Vec c;
+          if (at + C::kN <= hi) {
+            c = C::load(x + at);
+          } else {
+#pragma unroll
+            for (int e = 0; e < C::kN; ++e) c[e] = at + e < hi ? x[at + e] : (typename E::T)neg_inf();
+          }
+          if (order_of(chunk_max<E>(c)) <= above) continue;
+#pragma unroll
+          for (int e = 0; e < C::kN; ++e) {
+            const int o = order_of(E::get(c[e]));
+            if (o > above && at + e < hi) {
               const int f = atomicAdd(&n_found, 1);
               if (f < kFound) found[f] = key_of(o, (int)(at + e));
             }
           }
         }
         __syncthreads();
-        slow = n_found > kFound;
-        if (!slow) {
-          // every key's place among them, whatever order they came in
-          for (int i = tid; i < n_found; i += kLongThreads) {
-            const unsigned long long k = found[i];
-            int place = 0;
-            for (int f = 0; f < n_found; ++f) place += found[f] > k;
-            if (place < n) keys[place] = k;
+        return n_found;
+      };
+      int many_found = collect(bound > kNothing ? bound - 1 : bound);
+      if (many_found > kFound && bound != kNothing) {
+        // Too many are equal to the bound (a mask that leaves few scores: -inf): those above it, and the first ones that are equal
+        __syncthreads();
+        if (tid == 0) n_found = 0;
+        __syncthreads();
+        many_found = collect(bound);
+        int got = many_found;
+        for (int64_t from = lo; from < hi && got < n; from += kLongThreads) {
+          const bool hit = from + tid < hi && order_of(E::get(x[from + tid])) == bound;
+          const unsigned long long hits = __ballot(hit);
+          if (tid % 64 == 0) picked[tid / 64] = __popcll(hits);  // (not needed any more)
+          __syncthreads();
+          int before = got, all_hits = 0;
+          for (int w = 0; w < kWaves; ++w) {
+            before += w < tid / 64 ? picked[w] : 0;
+            all_hits += picked[w];
           }
+          before += __popcll(hits & ((1ull << (tid % 64)) - 1));
+          if (hit && before < n) keys[before] = key_of(bound, (int)(from + tid));
+          got += all_hits;
+          __syncthreads();
+        }
+      }
+      slow = many_found > kFound;
+      if (!slow) {
+        // every key's place among them, whatever order they came in
+        for (int i = tid; i < many_found; i += kLongThreads) {
+          const int place = place_of(found[i], found, many_found);
+          if (place < n) keys[place] = found[i];
         }
       }
     }
@@ -354,35 +405,47 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_long_kernel(LogprobsArg
   }
 }
 
-// The parts of a row (at most 64) as one, a wave per row: sums in the order of the parts, and the best of the parts' next keys, `top` times.
+// The parts of a row (at most 64) as one, a workgroup per row: sums in the order of the parts.  The parts' keys are falling, so that p + 1
+// of them reach a part's p-th: the bound is the m-th largest of the parts' p-th, m (p + 1) >= `top`, and what reaches it is sorted.
 template <class E>
-__global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsArgs a) {
-  __shared__ unsigned long long keys[kMaxTop];
+__global__ __launch_bounds__(kLongThreads) void logprobs_join_kernel(LogprobsArgs a) {
+  __shared__ unsigned long long keys[kMaxTop], all[64 * kMaxTop], heads[64], bound_;
+  __shared__ Sums sums;
+  __shared__ int n_all;
   const unsigned row = blockIdx.x, s = row / (unsigned)a.frames, t = row % (unsigned)a.frames;
   if (a.lengths && (int)t >= a.lengths[s]) return;
   const typename E::T *x = static_cast<const typename E::T *>(a.scores) + s * a.seq_stride + t * a.stride;
   const char *from = static_cast<const char *>(a.workspace) + (int64_t)row * a.splits * part_bytes(a.top);
-  Sums q = {neg_inf(), 0.0f, 0.0f};
-  const int lane = threadIdx.x;
-  if (lane < a.splits) q = reinterpret_cast<const Part *>(from + lane * part_bytes(a.top))->s;
-  const float m = max_over<64>(q.m);
-  grow(q, m);
-  q.sum = sum_over<64>(q.sum);
-  q.wsum = sum_over<64>(q.wsum);
-  const unsigned long long *mine = reinterpret_cast<const unsigned long long *>(from + lane * part_bytes(a.top) + 16);
-  int next = 0;
-  unsigned long long head = lane < a.splits && a.top ? mine[0] : 0;
-  for (int i = 0; i < a.top; ++i) {
-    unsigned long long k = head;
-    for (int d = 1; d < 64; d <<= 1) {
-      const unsigned long long o = __shfl_xor(k, d);
-      k = o > k ? o : k;
-    }
-    if (lane == 0) keys[i] = k;
-    if (head == k && k) head = ++next < a.top ? mine[next] : 0;
+  const int tid = threadIdx.x;
+  if (tid < 64) {
+    Sums q = {neg_inf(), 0.0f, 0.0f};
+    if (tid < a.splits) q = reinterpret_cast<const Part *>(from + tid * part_bytes(a.top))->s;
+    grow(q, max_over<64>(q.m));
+    q.sum = sum_over<64>(q.sum);
+    q.wsum = sum_over<64>(q.wsum);
+    if (tid == 0) { sums = q; bound_ = 0; n_all = 0; }
+  }
+  if (a.top) {
+    const int p = (a.top - 1) / a.splits, m = (a.top + p) / (p + 1);
+    unsigned long long k = 0;
+    if (tid < 64) heads[tid] = k = tid < a.splits ? reinterpret_cast<const unsigned long long *>(from + tid * part_bytes(a.top) + 16)[p] : 0;
+    __syncthreads();
+    if (tid < 64 && k && place_of(k, heads, 64) == m - 1) bound_ = k;
   }
   __syncthreads();
-  finish_row<E>(a, row, x, q, keys);
+  if (a.top) {
+    for (int i = tid; i < a.splits * a.top; i += kLongThreads) {
+      const unsigned long long k = reinterpret_cast<const unsigned long long *>(from + (i / a.top) * part_bytes(a.top) + 16)[i % a.top];
+      if (k && k >= bound_) all[atomicAdd(&n_all, 1)] = k;
+    }
+    __syncthreads();
+    for (int i = tid; i < n_all; i += kLongThreads) {
+      const int place = place_of(all[i], all, n_all);
+      if (place < a.top) keys[place] = all[i];
+    }
+    __syncthreads();
+  }
+  finish_row<E>(a, row, x, sums, keys);
 }
 
 // ---- the gradient

@@ -133,10 +133,10 @@ template <class E> int run_loglikes(const LoglikesArgs &a, bool direct, void *st
   return run_rows<E, 32, 512, 32, 64, 64, 4, 4, 2>(a, direct, stream);
 }
 
-// Long rows are cut until there are about 1,024 workgroups, into parts of 8,192 scores at least and 64 of them at most.
+// Long rows are cut until there are about 1,024 workgroups, into parts of 2,048 scores at least and 64 of them at most.
 int row_splits(int64_t rows, int32_t v) {
   if (v <= kShortRow) return 1;
-  const int64_t most = (v - 1) / 8192 + 1, want = (1024 - 1) / rows + 1;
+  const int64_t most = (v - 1) / 2048 + 1, want = (1024 - 1) / rows + 1;
   const int64_t n = want < most ? want : most;
   return (int)(n < 64 ? n : 64);
 }
@@ -153,7 +153,7 @@ template <class E> int run_logprobs(LogprobsArgs a, void *stream) {
   a.splits = row_splits(rows, a.v);
   a.split_size = ((a.v - 1) / a.splits / 8 + 1) * 8;
   const int rc = launch(me, logprobs_long_kernel<E>, rows * a.splits, kLongThreads, a, stream);
-  return rc != WFST_OK || a.splits == 1 ? rc : launch(me, logprobs_join_kernel<E>, rows, 64, a, stream);
+  return rc != WFST_OK || a.splits == 1 ? rc : launch(me, logprobs_join_kernel<E>, rows, kLongThreads, a, stream);
 }
 
 template <class E> int run_backward(BackwardArgs a, void *stream) {

@@ -460,6 +460,24 @@ def test_token_logprobs_strides_and_lengths(v, dt):
     check_logprobs(x[0], tokens[0, :, 0].contiguous(), 0)                          # one token per row
 
 
+@pytest.mark.parametrize("v", [2049, 40000, 130000])
+def test_token_logprobs_of_rows_that_leave_few_tokens(v):
+    """Fewer allowed tokens than alternatives asked for, here and there in the row; equal scores everywhere but for a few."""
+    g = gen(v, 44)
+    for rows in (3, 300):
+        x = torch.full((rows, v), -math.inf, device="cuda").bfloat16()
+        for i in range(rows):
+            for j in torch.randint(0, v, (i % 6,), generator=g, device="cuda").tolist():
+                x[i, j] = 1.0 + (j % 3)
+        y = torch.zeros((rows, v), device="cuda")
+        y[:, v // 3], y[:, v - 1], y[:, :40] = 1.0, 1.0, -1.0
+        z = torch.full((rows, v), -5.0, device="cuda")
+        z[:, 100:1400] = (torch.arange(1300, device="cuda") * 0.01).flip(0)          # more above the rest than are kept track of
+        for t in (x, y, z):
+            for top in (1, 5, 33, 64):
+                check_logprobs(t, some_tokens(g, rows, v, 1), top)
+
+
 def test_token_logprobs_far_from_zero_and_sure_rows():
     for base in (3000.0, -3000.0, 60000.0):
         x = torch.full((4, 1000), base, device="cuda") + randn(gen(1), 4, 1000) * 3
