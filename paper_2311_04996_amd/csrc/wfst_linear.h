@@ -86,11 +86,9 @@ __device__ __forceinline__ void store8(void *p, int64_t i, int dtype, int count,
   }
 }
 
-// what follows the product sums v of columns col.. of row m
-__device__ __forceinline__ void finish(const LinearArgs &a, int64_t m, int col, float (&v)[8], const float (&bias)[8]) {
+// what follows the sums v (product and bias) of columns col.. of row m
+__device__ __forceinline__ void finish(const LinearArgs &a, int64_t m, int col, float (&v)[8]) {
   const int count = a.n - col;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] += bias[e];
   if (a.activation == 1) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = activate(v[e], 1);
@@ -101,8 +99,10 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int64_t m, int col, 
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = activate(v[e], 3);
   }
+  if (a.scale != 1.0f) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+    for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+  }
   if (a.residual) {
     float r[8];
     load8(a.residual, m * a.residual_stride + col, a.out_dtype, count, r);
@@ -278,17 +278,22 @@ struct Tile {
   }
   // The whole product.  Ends with all waves done with LDS.  (STAGES parts behind the last one are loaded too, while the last ones
   // are multiplied, and not used: so every wait has the same number of loads behind it.)  used: a bit per group, whether this
-  // wave's sums of it are (uniform).
-  __device__ __forceinline__ void product(Buffer x, Buffer w, char *const (&stage)[STAGES], int k_bytes, Sums &acc, unsigned used = ~0u) {
+  // wave's sums of it are (uniform).  before, after: what is to be done while the first parts are on their way, before and behind a meeting
+  // of the waves; `after` puts the sums to what they begin with.
+  template <class Before, class After>
+  __device__ __forceinline__ void product(Buffer x, Buffer w, char *const (&stage)[STAGES], int k_bytes, Sums &acc, Before before, After after,
+                                          unsigned used = ~0u) {
     static_assert(kTurn % GROUPS == 0 && kTurn % STAGES == 0, "a turn ends where it began");
     constexpr int kStep = kTurn / GROUPS;            // parts of k in a turn
     const int parts = (k_bytes + ROW - 1) / ROW;
     Step f[2];
 #pragma unroll
     for (int i = 0; i < STAGES; ++i) load(x, w, stage[i], i / GROUPS, i % GROUPS);
+    before();
     wait_loads<(STAGES - 1) * kLoads>();
     meet();
     read(f[0], stage[0], 0);
+    after();
     int k = 0;
     for (; k + kStep < parts; k += kStep) turn<0, false>(k, parts, k_bytes, x, w, stage, f, acc, used);
     for (; k < parts; k += kStep) turn<0, true>(k, parts, k_bytes, x, w, stage, f, acc, used);
@@ -311,9 +316,9 @@ struct Tile {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) *reinterpret_cast<i32x4 *>(stage + piece(i) * 1024 + (threadIdx.x & 63) * 16) = reg[i];
   }
-  template <class RowOf>
+  template <class RowOf, class Before, class After>
   static __device__ __forceinline__ void product_staged(RowOf row_of, int64_t group, int rows_w, char *s0, char *s1, int k_bytes, Sums &acc,
-                                                        unsigned used = ~0u) {
+                                                        Before before, After after, unsigned used = ~0u) {
     constexpr int kTwo = GROUPS % 2 == 0 ? GROUPS : 2 * GROUPS;                 // parts in a turn of two stages
     const int parts = (k_bytes + ROW - 1) / ROW;
     const char *from[kLoads];
@@ -322,8 +327,10 @@ struct Tile {
     i32x4 ahead[2][kLoads];                            // the next two parts, on their way
     fetch(ahead[0], from, 0, 0, group, rows_w, k_bytes);
     fetch(ahead[1], from, 1 / GROUPS, 1 % GROUPS, group, rows_w, k_bytes);
+    before();
     put(s0, ahead[0]);
     meet();
+    after();
     for (int k = 0; k < parts; k += kTwo / GROUPS) {
 #pragma unroll
       for (int i = 0; i < kTwo; ++i) {
@@ -351,31 +358,50 @@ __device__ __forceinline__ int64_t tile_of(int64_t block, int64_t tiles) {
 
 // DIRECT: rows of x and w start at multiples of 16 bytes and are whole chunks, and a tile's rows lie within 2 GB
 template <class E, int BM, int BN, int WM, int WN, int ROW, bool DIRECT>
-__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_kernel(LinearArgs a) {
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), (BM / WM) * (BN / WN) >= 8 ? 4 : 3) void linear_kernel(LinearArgs a) {
   using T = Tile<E, BM, BN, WM, WN, ROW>;
   constexpr int kPitch = WN + 4;                        // floats; 32 rows of it per wave in the epilogue
   constexpr int kWaveOut = 32 * kPitch * 4, kPer = (T::kWaves + 2) / 3;      // waves per stage there
   constexpr int kLds = T::kStage > kWaveOut * kPer ? T::kStage : kWaveOut * kPer;
+  static_assert(T::kThreads >= BN, "a thread per column");
   __shared__ __align__(16) char s0[kLds], s1[kLds], s2[kLds];
+  __shared__ __align__(16) float bias[BN];
   const int64_t tile = tile_of(blockIdx.x, gridDim.x);
   const int64_t m0 = tile / a.tiles_n * BM;
   const int n0 = (int)(tile % a.tiles_n) * BN;
   const char *x = static_cast<const char *>(a.x), *w = static_cast<const char *>(a.w);
   constexpr int kSize = (int)sizeof(typename E::T);
-  typename T::Sums sums = {};
+  typename T::Sums sums;
   f32x16 (&acc)[T::kTN][T::kTM] = sums[0];
+  // The sums begin with the bias, which comes while the first parts do: the epilogue, which nothing hides, is shorter for it.
+  const int my = threadIdx.x;
+  const float my_bias = a.bias && my < BN && n0 + my < a.n ? load_as(a.bias, n0 + my, a.bias_dtype) : 0.0f;
+  const auto before = [&] { if (my < BN) bias[my] = my_bias; };
+  const auto after = [&] {
+    const int c0 = (threadIdx.x >> 6) % T::kWavesN * WN + 4 * ((threadIdx.x & 63) >> 5);
+#pragma unroll
+    for (int i = 0; i < T::kTN; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 b = *reinterpret_cast<const f32x4 *>(bias + c0 + 32 * i + 8 * q);
+#pragma unroll
+        for (int j = 0; j < T::kTM; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = b[e];
+      }
+  };
   const char *xt = x + m0 * a.x_stride * kSize, *wt = w + (int64_t)n0 * a.w_stride * kSize;   // the tile's first rows
   if (DIRECT) {
     T t;
     t.aim([&](int r) { return r < BM ? r * (int)a.x_stride * kSize : (r - BM) * (int)a.w_stride * kSize; }, 0);
     char *const stage[3] = {s0, s1, s2};
     t.product(buffer(xt, bytes_behind(a.rows - m0, a.x_stride, a.k, kSize)), buffer(wt, bytes_behind(a.n - n0, a.w_stride, a.k, kSize)), stage,
-              a.k * kSize, sums);
+              a.k * kSize, sums, before, after);
   } else {
     T::product_staged([&](int r) {
       const int64_t m = m0 + r < a.rows ? r : a.rows - 1 - m0, n = n0 + (r - BM) < a.n ? r - BM : a.n - 1 - n0;
       return r < BM ? xt + m * a.x_stride * kSize : wt + n * a.w_stride * kSize;
-    }, 0, 0, s0, s1, a.k * kSize, sums);
+    }, 0, 0, s0, s1, a.k * kSize, sums, before, after);
   }
 
   // Epilogue: 32 rows at a time go through the wave's own part of LDS, so that a lane gets 8 neighbouring columns of a row.
@@ -385,9 +411,6 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_kernel(L
   const int64_t mw = m0 + (wave / T::kWavesN) * WM;
   constexpr int kLanes = WN / 8, kRows = 64 / kLanes;   // lanes per row, rows at a time
   const int col = nw + (lane % kLanes) * 8;
-  float bias[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) bias[e] = a.bias && col + e < a.n ? load_as(a.bias, col + e, a.bias_dtype) : 0.0f;
 #pragma unroll
   for (int j = 0; j < T::kTM; ++j) {
 #pragma unroll
@@ -405,7 +428,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_kernel(L
       const float *z = out + (r + lane / kLanes) * kPitch + (lane % kLanes) * 8;
       const f32x4 z0 = *reinterpret_cast<const f32x4 *>(z), z1 = *reinterpret_cast<const f32x4 *>(z + 4);
       float v[8] = {z0[0], z0[1], z0[2], z0[3], z1[0], z1[1], z1[2], z1[3]};
-      if (m < a.rows && col < a.n) finish(a, m, col, v, bias);
+      if (m < a.rows && col < a.n) finish(a, m, col, v);
     }
     __builtin_amdgcn_wave_barrier();
   }
@@ -464,7 +487,9 @@ __global__ __launch_bounds__(512) void linear_few_kernel(LinearArgs a) {
     for (int e = 0; e < 8; ++e) v[e] += part[i][r][col + e];
 #pragma unroll
   for (int e = 0; e < 8; ++e) bias[e] = a.bias && n0 + col + e < a.n ? load_as(a.bias, n0 + col + e, a.bias_dtype) : 0.0f;
-  finish(a, m0 + r, n0 + col, v, bias);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] += bias[e];
+  finish(a, m0 + r, n0 + col, v);
 }
 
 // ---- wfst_loglikes
@@ -578,7 +603,16 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), PER_SIMD) void loglikes
     my_bias[i] = a.bias && c < a.v ? load_as(a.bias, c, a.bias_dtype) : 0.0f;
     my_prior[i] = a.log_prior && c < a.v ? a.log_prior[c] : 0.0f;
   }
-  typename T::Sums acc = {};
+  typename T::Sums acc;
+  const auto nothing = [] {};
+  const auto zero = [&] {
+#pragma unroll
+    for (int h = 0; h < GROUPS; ++h)
+#pragma unroll
+      for (int i = 0; i < T::kTN; ++i)
+#pragma unroll
+        for (int j = 0; j < T::kTM; ++j) acc[h][i][j] = f32x16{};
+  };
   if (DIRECT) {
     T t;
     t.aim([&](int r) { return (int)(r < BM ? x_at[r] : w_offset(r)); }, BN * (int)a.w_stride * kSize);
@@ -587,9 +621,9 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), PER_SIMD) void loglikes
     char *stage[STAGES];
 #pragma unroll
     for (int i = 0; i < STAGES; ++i) stage[i] = all[i];
-    t.product(buffer(x, (uint32_t)(x_end * kSize)), buffer(w, bytes_behind(a.v, a.w_stride, a.k, kSize)), stage, a.k * kSize, acc, used);
+    t.product(buffer(x, (uint32_t)(x_end * kSize)), buffer(w, bytes_behind(a.v, a.w_stride, a.k, kSize)), stage, a.k * kSize, acc, nothing, zero, used);
   } else {
-    T::product_staged([&](int r) { return r < BM ? x + x_at[r] : w + w_offset(r); }, BN * a.w_stride * kSize, a.v, s0, s1, a.k * kSize, acc, used);
+    T::product_staged([&](int r) { return r < BM ? x + x_at[r] : w + w_offset(r); }, BN * a.w_stride * kSize, a.v, s0, s1, a.k * kSize, acc, nothing, zero, used);
   }
 
 #pragma unroll
