@@ -24,7 +24,7 @@ int refuse(const char *what, const char *why) {
 template <class Args>
 int launch(const char *what, void (*kernel)(Args), int64_t workgroups, int threads, const Args &a, void *stream) {
   if (workgroups <= 0) return WFST_OK;
-  if (workgroups > INT_MAX) return refuse(what, "too many rows for one launch");
+  if (workgroups > UINT32_MAX / threads) return refuse(what, "too many rows for one launch");      // (a grid has 2^32 - 1 work items at most)
   Args copy = a;
   void *argv[] = {&copy};
   const hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)workgroups), dim3(threads), argv, 0,

@@ -102,7 +102,7 @@ class Lattice:
     def path_logprobs(self, scores, paths, top=0, stream=None):
         """How sure the model was of the labels of n paths, frame by frame: token_logprobs of scores (CUDA [num_frames,
         V], the model's logits or log-likelihoods) at the paths' labels: logprobs [num_frames, n], and of every frame lse,
-        entropy and the `top` best labels.  paths: lists of link indices, as nbest gives them."""
+        entropy and the `top` best labels.  paths: at most 256 lists of link indices, as nbest gives them."""
         import torch
         from .binding import _on
         from .outputs import token_logprobs

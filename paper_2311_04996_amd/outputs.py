@@ -67,6 +67,8 @@ def _matrix(t, what):
         raise ValueError(f"the last dimension of {what} must be contiguous")
     if len(st) == 2:
         return t.shape[0], st[0]
+    if t.numel() == 0:
+        return 0, t.shape[-1]
     rows, stride = 1, t.shape[-1]
     for size, s in zip(reversed(t.shape[:-1]), reversed(st[:-1])):
         if size == 1:

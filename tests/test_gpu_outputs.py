@@ -174,6 +174,8 @@ def test_linear_refuses_what_does_not_fit():
         with pytest.raises(ValueError):
             linear(a, c)
     assert linear(x[:0], w).shape == (0, 6)
+    for lead in ((0, 4), (4, 0), (3, 0, 2)):
+        assert linear(torch.zeros(*lead, 8, device="cuda"), w).shape == (*lead, 6)
     with pytest.raises(WfstError):
         linear(x[:, :0], w[:, :0])
 

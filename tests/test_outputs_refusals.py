@@ -90,6 +90,12 @@ def test_token_logprobs_refuses(lib, kw, word):
     refused(lib, "wfst_token_logprobs", tlp(**kw), word)
 
 
+def test_more_rows_than_a_launch_has_are_refused(lib):
+    big = dict(seqs=1 << 15, frames=1 << 15, v=2, stride=0, seq_stride=0, given=0, top=0, lengths=None)      # 2^30 rows that share two scores
+    refused(lib, "wfst_token_logprobs", tlp(logprobs=None, tokens=None, lse=None, entropy=A << 8, maximum=A << 9, log_sum=A << 10, **big), "too many rows")
+    refused(lib, "wfst_linear", lin(rows=1 << 34, x_stride=0, residual=None, y=A << 12), "too many rows")
+
+
 def test_token_logprobs_needs_its_workspace(lib):
     for rows, v, top in ((1, 128000, 8), (4, 128000, 0), (1, 1 << 30, 64), (30, 65536, 8)):
         need = lib.wfst_token_logprobs_workspace(rows, v, top)
