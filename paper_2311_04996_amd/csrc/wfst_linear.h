@@ -357,14 +357,14 @@ __device__ __forceinline__ int64_t tile_of(int64_t block, int64_t tiles) {
 }
 
 // DIRECT: rows of x and w start at multiples of 16 bytes and are whole chunks, and a tile's rows lie within 2 GB
-template <class E, int BM, int BN, int WM, int WN, int ROW, bool DIRECT>
-__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), (BM / WM) * (BN / WN) >= 8 ? 4 : 3) void linear_kernel(LinearArgs a) {
-  using T = Tile<E, BM, BN, WM, WN, ROW>;
+template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES, bool DIRECT>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), (BM / WM) * (BN / WN) >= 8 ? 4 : (BM / WM) * (BN / WN) >= 4 ? 3 : 1) void linear_kernel(LinearArgs a) {
+  using T = Tile<E, BM, BN, WM, WN, ROW, STAGES>;
   constexpr int kPitch = WN + 4;                        // floats; 32 rows of it per wave in the epilogue
-  constexpr int kWaveOut = 32 * kPitch * 4, kPer = (T::kWaves + 2) / 3;      // waves per stage there
+  constexpr int kWaveOut = 32 * kPitch * 4, kPer = (T::kWaves + STAGES - 1) / STAGES;      // waves per stage there
   constexpr int kLds = T::kStage > kWaveOut * kPer ? T::kStage : kWaveOut * kPer;
   static_assert(T::kThreads >= BN, "a thread per column");
-  __shared__ __align__(16) char s0[kLds], s1[kLds], s2[kLds];
+  __shared__ __align__(16) char s0[kLds], s1[kLds], s2[kLds], s3[STAGES > 3 ? kLds : 16];
   __shared__ __align__(16) float bias[BN];
   const int64_t tile = tile_of(blockIdx.x, gridDim.x);
   const int64_t m0 = tile / a.tiles_n * BM;
@@ -394,7 +394,10 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), (BM / WM) * (BN / WN) >
   if (DIRECT) {
     T t;
     t.aim([&](int r) { return r < BM ? r * (int)a.x_stride * kSize : (r - BM) * (int)a.w_stride * kSize; }, 0);
-    char *const stage[3] = {s0, s1, s2};
+    char *const all[4] = {s0, s1, s2, s3};
+    char *stage[STAGES];
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) stage[i] = all[i];
     t.product(buffer(xt, bytes_behind(a.rows - m0, a.x_stride, a.k, kSize)), buffer(wt, bytes_behind(a.n - n0, a.w_stride, a.k, kSize)), stage,
               a.k * kSize, sums, before, after);
   } else {
@@ -406,7 +409,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), (BM / WM) * (BN / WN) >
 
   // Epilogue: 32 rows at a time go through the wave's own part of LDS, so that a lane gets 8 neighbouring columns of a row.
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float *out = reinterpret_cast<float *>((wave / kPer == 0 ? s0 : wave / kPer == 1 ? s1 : s2) + (wave % kPer) * kWaveOut);
+  float *out = reinterpret_cast<float *>((wave / kPer == 0 ? s0 : wave / kPer == 1 ? s1 : wave / kPer == 2 ? s2 : s3) + (wave % kPer) * kWaveOut);
   const int nw = n0 + (wave % T::kWavesN) * WN;
   const int64_t mw = m0 + (wave / T::kWavesN) * WM;
   constexpr int kLanes = WN / 8, kRows = 64 / kLanes;   // lanes per row, rows at a time

@@ -71,34 +71,42 @@ template <class F> int by_type(int32_t dtype, F f) { return dtype == 0 ? f(F32{}
 
 int64_t count_tiles(const LinearArgs &a, int bm, int bn) { return ((a.rows - 1) / bm + 1) * (((int64_t)a.n - 1) / bn + 1); }
 
-template <class E, int BM, int BN, int WM, int WN, int ROW, bool DIRECT>
+template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES, bool DIRECT>
 int run_tiles(LinearArgs a, void *stream) {
   a.tiles_n = (a.n - 1) / BN + 1;
   if ((a.rows - 1) / BM + 1 > INT_MAX / a.tiles_n) return refuse("wfst_linear", "too many rows for one launch");
-  return launch("wfst_linear", linear_kernel<E, BM, BN, WM, WN, ROW, DIRECT>, count_tiles(a, BM, BN), 64 * (BM / WM) * (BN / WN), a, stream);
+  return launch("wfst_linear", linear_kernel<E, BM, BN, WM, WN, ROW, STAGES, DIRECT>, count_tiles(a, BM, BN), 64 * (BM / WM) * (BN / WN), a, stream);
 }
 
 // The largest tile of which there is one for each compute unit: it reads the least per product (256 x 256: 32 bytes per clock and
 // compute unit at full rate, 128 x 128: 64, which is what a compute unit can load), but smaller ones fill the GPU earlier.
-// bf16, us, tiles of 256 x 256 / 256 x 128 / 128 x 128 / 64 x 64 (k x n): 118,417 rows, 512 x 2048: 279 / 300 / 331 / -;
+// bf16, us, inputs in the caches, tiles of 256 x 256 / 256 x 128 / 128 x 128 / 64 x 64 (k x n): 118,417 rows, 512 x 2048: 279 / 300 / 331 / -;
 // 16,384, 2048 x 512: 49 / 44 / 47 / 57 (128, 256, 512, 2,048 tiles); 2,048, 2048 x 2048: 44 / 35 / 28 / 39 (64, 128, 256, 1,024);
-// 512, 512 x 2048: 18 / 13 / 10 / 6.  Single tiles of 16 x 16 with k shared out over the waves: 33 to 128 rows, 2048 x 512: 7.4, 64 x 64: 9.1;
-// 512 rows (1,024 tiles): 19, 64 x 64: 9.3.  In fp32 the matrix instructions bound the kernel and the larger tiles gain nothing
-// (14,803 rows, 512 x 2048: 268 / 251 / 255 / 264), nor does 256 x 256 by way of registers (511 x 2047: 482 / 476 / 531 / 931).
+// 512, 512 x 2048: 18 / 13 / 10 / 6.  Half of a 64 x 64 tile, as long as there is a compute unit for each: 1,024 rows, 2048 x 512, inputs from
+// memory: 10.2, whole ones 12.2; behind that (512 x 2048): 13.8, 9.4.  Tiles of 16 x 16 with k shared out over the waves: 33 to 128 rows,
+// 2048 x 512: 7.4, 64 x 64: 9.1; 512 rows (1,024 tiles): 19, 64 x 64: 9.3.  By way of registers 256 x 256 gains nothing (511 x 2047: 482 / 476 / 531).
+// In fp32 the matrix instructions take longest, and 128 x 128 is taken where it leaves at most an eighth of the last round idle: 64 x 64 /
+// 128 x 128 at 14,803 rows, 176 x 320 (348 tiles of 128 x 128): 22 / 31, by way of registers 177 x 333: 32 / 40; 512 x 512 (464): 87 / 79;
+// 512 x 2048 (1,856): 273 / 275.
 template <class E> int run_linear(LinearArgs a, bool direct, void *stream) {
-  constexpr bool kHalf = sizeof(typename E::T) == 2;
   if (count_tiles(a, 16, 16) <= 256) {
     a.tiles_n = (a.n - 1) / 16 + 1;
     return launch("wfst_linear", linear_few_kernel<E>, count_tiles(a, 16, 16), 512, a, stream);
   }
-  if constexpr (kHalf) {
-    if (direct && count_tiles(a, 256, 256) >= 256) return run_tiles<E, 256, 256, 64, 64, 64, true>(a, stream);
+  if constexpr (sizeof(typename E::T) == 4) {
+    const int64_t tiles = count_tiles(a, 128, 128), rounds = (tiles + 255) / 256;
+    if (tiles >= 256 && tiles * 8 >= rounds * 256 * 7)
+      return direct ? run_tiles<E, 128, 128, 64, 64, 64, 3, true>(a, stream) : run_tiles<E, 128, 128, 64, 64, 64, 3, false>(a, stream);
+    return direct ? run_tiles<E, 64, 64, 32, 32, 64, 4, true>(a, stream) : run_tiles<E, 64, 64, 32, 32, 64, 3, false>(a, stream);
+  } else {
+    if (direct && count_tiles(a, 256, 256) >= 256) return run_tiles<E, 256, 256, 64, 64, 64, 3, true>(a, stream);
     if (count_tiles(a, 256, 128) >= 256)
-      return direct ? run_tiles<E, 256, 128, 64, 64, 64, true>(a, stream) : run_tiles<E, 256, 128, 64, 64, 64, false>(a, stream);
+      return direct ? run_tiles<E, 256, 128, 64, 64, 64, 3, true>(a, stream) : run_tiles<E, 256, 128, 64, 64, 64, 3, false>(a, stream);
+    if (count_tiles(a, 128, 128) >= 256)
+      return direct ? run_tiles<E, 128, 128, 64, 64, 64, 3, true>(a, stream) : run_tiles<E, 128, 128, 64, 64, 64, 3, false>(a, stream);
+    if (direct && count_tiles(a, 32, 64) <= 256) return run_tiles<E, 32, 64, 32, 32, 128, 4, true>(a, stream);
+    return direct ? run_tiles<E, 64, 64, 32, 32, 128, 3, true>(a, stream) : run_tiles<E, 64, 64, 32, 32, 128, 3, false>(a, stream);
   }
-  if (count_tiles(a, 128, 128) >= 256)
-    return direct ? run_tiles<E, 128, 128, 64, 64, 64, true>(a, stream) : run_tiles<E, 128, 128, 64, 64, 64, false>(a, stream);
-  return direct ? run_tiles<E, 64, 64, 32, 32, 128, true>(a, stream) : run_tiles<E, 64, 64, 32, 32, 128, false>(a, stream);
 }
 
 template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES, int GROUPS, int PER_SIMD>
