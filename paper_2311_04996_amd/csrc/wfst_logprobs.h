@@ -95,9 +95,26 @@ __device__ __forceinline__ float given_logprob(const typename E::T *x, int v, in
   return logprob_of(E::get(x[token]), m, ls);
 }
 
+// How many of n keys are above k (n reads in flight, not one after the other)
+__device__ __forceinline__ int place_of(unsigned long long k, const unsigned long long *keys, int n) {
+  int place = 0, f = 0;
+  for (; f + 8 <= n; f += 8)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) place += keys[f + i] > k;
+  for (; f < n; ++f) place += keys[f] > k;
+  return place;
+}
+
+// Between a wave's writes to LDS and its reads of them: they are carried out in order, the compiler has to leave them so.
+__device__ __forceinline__ void in_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ---- rows of up to 2,048 scores: LANES lanes hold a row, EACH scores per lane, in registers.  16 lanes for up to 256: a reduction
 // then stays within the rotations, and serves four rows.
-template <class E, int LANES, int EACH>
+template <class E, int LANES, int EACH, bool MANY>
 __global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a) {
   const int lane = threadIdx.x % LANES;
   const unsigned row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, rows = (unsigned)a.seqs * a.frames;
@@ -130,10 +147,55 @@ __global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a) {
         a.logprobs[(int64_t)row * a.given + g] = given_logprob<E>(x, a.v, a.tokens[(int64_t)row * a.given + g], m, ls);
   }
   if (a.top == 0) return;
-  // The top ones, one after the other: every lane's best, the best of them, and its lane goes on to its next one.
   int order[EACH];
 #pragma unroll
-  for (int e = 0; e < EACH; ++e) order[e] = lane + LANES * e < a.v ? order_of(z[e]) : kNothing;
+  for (int e = 0; e < EACH; ++e) order[e] = live && lane + LANES * e < a.v ? order_of(z[e]) : kNothing;
+  if constexpr (MANY) {
+    // The top-th largest of the lanes' maxima is a bound that as many scores reach; what reaches it is listed and finds its place there.
+    constexpr int kList = LANES == 64 ? 128 : 64;
+    __shared__ __align__(16) int maxima[256 / LANES][LANES];
+    __shared__ unsigned long long list[256 / LANES][kList];
+    __shared__ int bounds[256 / LANES];
+    const int group = threadIdx.x / LANES;
+    int own = order[0], rank = 0, mine = 0;
+#pragma unroll
+    for (int e = 1; e < EACH; ++e) own = order[e] > own ? order[e] : own;
+    maxima[group][lane] = own;
+    in_order();
+#pragma unroll
+    for (int i = 0; i < LANES; i += 4) {
+      const int4 o = *reinterpret_cast<const int4 *>(&maxima[group][i]);
+      rank += (o.x > own || (o.x == own && i < lane)) + (o.y > own || (o.y == own && i + 1 < lane)) + (o.z > own || (o.z == own && i + 2 < lane)) +
+              (o.w > own || (o.w == own && i + 3 < lane));
+    }
+    if (rank == a.top - 1) bounds[group] = own;
+    in_order();
+    const int bound = bounds[group] > kNothing ? bounds[group] : kNothing + 1;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) mine += order[e] >= bound;
+    int to = mine;                                     // the lanes' lists lie one behind the other
+    for (int d = 1; d < LANES; d <<= 1) {
+      const int o = __shfl_up(to, d, LANES);
+      to += lane >= d ? o : 0;
+    }
+    const int total = __shfl(to, LANES - 1, LANES);
+    to -= mine;
+    if (!__any(total > kList)) {                       // (else too many are equal)
+#pragma unroll
+      for (int e = 0; e < EACH; ++e)
+        if (order[e] >= bound) list[group][to++] = key_of(order[e], lane + LANES * e);
+      in_order();
+      for (int i = lane; i < total && live; i += LANES) {
+        const unsigned long long key = list[group][i];
+        const int place = place_of(key, list[group], total);
+        if (place >= a.top) continue;
+        if (a.top_ids) a.top_ids[(int64_t)row * a.top + place] = index_of(key);
+        if (a.top_logprobs) a.top_logprobs[(int64_t)row * a.top + place] = logprob_of(score_of(key), m, ls);
+      }
+      return;
+    }
+  }
+  // One after the other: every lane's best, the best of them, and its lane goes on to its next one.
   for (int i = 0; i < a.top; ++i) {
     int best = order[0], at = 0;
 #pragma unroll
@@ -221,16 +283,6 @@ __device__ __forceinline__ void finish_row(const LogprobsArgs &a, int64_t row, c
     if (a.top_ids) a.top_ids[row * a.top + i] = index_of(keys[i]);
     if (a.top_logprobs) a.top_logprobs[row * a.top + i] = logprob_of(score_of(keys[i]), s.m, ls);
   }
-}
-
-// How many of n keys are above k (n reads in flight, not one after the other)
-__device__ __forceinline__ int place_of(unsigned long long k, const unsigned long long *keys, int n) {
-  int place = 0, f = 0;
-  for (; f + 8 <= n; f += 8)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) place += keys[f + i] > k;
-  for (; f < n; ++f) place += keys[f] > k;
-  return place;
 }
 
 template <class E>

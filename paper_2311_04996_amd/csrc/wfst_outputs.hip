@@ -149,15 +149,24 @@ int row_splits(int64_t rows, int32_t v) {
   return (int)(n < 64 ? n : 64);
 }
 
+template <class E, int LANES, int EACH> int run_short(const LogprobsArgs &a, int64_t rows, void *stream) {
+  // One after the other costs a reduction each; a bound and a sorted list cost as much as about six of them, over 64 lanes eight, whatever
+  // the number, until most lanes' maxima are in the list.  fp32, us one after the other / by a bound: 118,417 rows of 129: top 4 29 / 31,
+  // 6 39 / 33, 12 56 / 40, 16 67 / 69; 14,800 rows of 2,048: top 4 49 / 64, 8 69 / 65, 16 104 / 68, 48 250 / 88.
+  const bool many = a.top >= (LANES == 16 ? 6 : 8) && a.top <= LANES * 3 / 4;
+  return launch("wfst_token_logprobs", many ? logprobs_short_kernel<E, LANES, EACH, true> : logprobs_short_kernel<E, LANES, EACH, false>,
+                (rows - 1) / (256 / LANES) + 1, 256, a, stream);
+}
+
 template <class E> int run_logprobs(LogprobsArgs a, void *stream) {
   const char *me = "wfst_token_logprobs";
   const int64_t rows = (int64_t)a.seqs * a.frames;
-  if (a.v <= 64) return launch(me, logprobs_short_kernel<E, 16, 4>, (rows - 1) / 16 + 1, 256, a, stream);
-  if (a.v <= 160) return launch(me, logprobs_short_kernel<E, 16, 10>, (rows - 1) / 16 + 1, 256, a, stream);
-  if (a.v <= 256) return launch(me, logprobs_short_kernel<E, 16, 16>, (rows - 1) / 16 + 1, 256, a, stream);
-  if (a.v <= 512) return launch(me, logprobs_short_kernel<E, 64, 8>, (rows - 1) / 4 + 1, 256, a, stream);
-  if (a.v <= 1024) return launch(me, logprobs_short_kernel<E, 64, 16>, (rows - 1) / 4 + 1, 256, a, stream);
-  if (a.v <= kShortRow) return launch(me, logprobs_short_kernel<E, 64, 32>, (rows - 1) / 4 + 1, 256, a, stream);
+  if (a.v <= 64) return run_short<E, 16, 4>(a, rows, stream);
+  if (a.v <= 160) return run_short<E, 16, 10>(a, rows, stream);
+  if (a.v <= 256) return run_short<E, 16, 16>(a, rows, stream);
+  if (a.v <= 512) return run_short<E, 64, 8>(a, rows, stream);
+  if (a.v <= 1024) return run_short<E, 64, 16>(a, rows, stream);
+  if (a.v <= kShortRow) return run_short<E, 64, 32>(a, rows, stream);
   a.splits = row_splits(rows, a.v);
   a.split_size = ((a.v - 1) / a.splits / 8 + 1) * 8;
   const int rc = launch(me, logprobs_long_kernel<E>, rows * a.splits, kLongThreads, a, stream);

@@ -395,7 +395,7 @@ def test_token_logprobs(v, dt):
 
 
 @pytest.mark.parametrize("dt", DT)
-@pytest.mark.parametrize("rows,v", [(300, 129), (1000, 29), (40, 5000), (600, 2100)])
+@pytest.mark.parametrize("rows,v", [(300, 129), (1000, 29), (50, 16), (50, 256), (90, 300), (90, 2048), (40, 5000), (600, 2100)])
 def test_token_logprobs_with_many_ties(rows, v, dt):
     """Scores of a few values: the top ones are the lowest indices of the highest value; rising and falling rows, too."""
     g = gen(rows, v)
@@ -404,8 +404,33 @@ def test_token_logprobs_with_many_ties(rows, v, dt):
     x[1, ::2] = 0.0                                                                # +0 and -0 are equal
     x[2], x[3] = torch.arange(v, device="cuda") * (8 / v), torch.arange(v, device="cuda") * (-8 / v)
     x[4] = torch.finfo(DT[dt]).min
-    for top in (1, 7, min(v, 64)):
+    for top in (1, 4, 7, 16, min(v, 64)):
         check_logprobs(x, some_tokens(g, rows, v, 1), top)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("v,top", [(16, 12), (29, 6), (129, 5), (129, 6), (129, 12), (129, 13), (256, 9), (300, 8), (1000, 48), (2048, 49), (2048, 20)])
+def test_token_logprobs_of_several_top_ones(v, top, dt):
+    """Numbers of top ones about those where the way they are found changes; padding, masked and ill rows beside ordinary ones."""
+    g = gen(v, top)
+    B, T = 5, 7
+    lengths = torch.tensor([7, 0, 3, 6, 1], dtype=torch.int32, device="cuda")
+    valid = torch.arange(T, device="cuda")[None] < lengths[:, None]
+    x = (randn(g, B, T, v) * 3).to(DT[dt])
+    x[~valid] = math.nan
+    x[0, 1] = -math.inf
+    x[0, 2, :-2] = -math.inf
+    x[0, 4] = torch.finfo(DT[dt]).min
+    x[3, 1, ::3] = -math.inf
+    r = check_logprobs(x, some_tokens(g, B * T, v, 2).view(B, T, 2), top, valid, lengths)
+    for t in r:
+        assert bool((t[~valid] == 0).all())
+    x = randn(g, 6, v).to(DT[dt])
+    x[2, v // 2], x[4, 1], x[4, 5] = math.nan, math.inf, math.nan
+    ids = token_logprobs(x, top=top).top_ids.long()
+    order = torch.where(torch.isnan(x), torch.full_like(x, math.inf), x)           # a NaN counts as above all, a lone one as an infinity here
+    order[4, 1] = torch.finfo(DT[dt]).max
+    assert torch.equal(ids, torch.sort(order, dim=-1, descending=True, stable=True).indices[:, :top])
 
 
 @pytest.mark.parametrize("dt", DT)
