@@ -22,20 +22,40 @@ struct LinearArgs {
   int32_t tiles_n;               // tiles along n; the grid has tiles_n times the tiles along the rows
 };
 
-// relu, silu and gelu as the header defines them; a NaN stays one
-__device__ __forceinline__ float activate(float z, int act) {
-  if (act == 1) return z < 0.0f ? 0.0f : z;
-  if (act == 2) return z * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));   // (the hardware's 1 / x is within 1 ulp)
-  if (act == 3) {
-    // 1 + erf(u), u = z / sqrt 2: erfc(|u|) by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (within 1.5e-7;
-    // the library's erff took 7.5 us of 47 at 14,803 x 177 x 333 in fp32, this takes 3)
-    const float u = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, u, 1.0f));
-    float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
-    p = __builtin_fmaf(p, t, 1.421413741f);
-    p = __builtin_fmaf(p, t, -0.284496736f);
-    p = __builtin_fmaf(p, t, 0.254829592f) * t * exp_fast(-u * u);
+// p(x) by Horner's rule, coefficients from the constant one on
+template <int N> __device__ __forceinline__ float horner(const float (&c)[N], float x) {
+  float p = c[N - 1];
+#pragma unroll
+  for (int i = N - 2; i >= 0; --i) p = __builtin_fmaf(p, x, c[i]);
+  return p;
+}
+
+// gelu: z / 2 erfc(-z / sqrt 2).  With a = |z|: erfc(a / sqrt 2) = e^(-a^2 / 2) F(a), and F, which falls from 1 like 0.8 / a, is a
+// polynomial in t = 1 / (1 + 0.35 a), fitted to the least relative error over a <= 16 (e^-128 is 0 in fp32), so that the lower tail
+// has as many digits as the rest.
+// FINE, for fp32 results: within 8 (z < 0) and 2.5 (z > 0) times 2^-24 of itself, by an odd polynomial for erf below a = 1 (1 - F e^..
+// would lose digits near 0) and the exponent with what its square lost.  Else, for a result that is rounded to 16 bits: within 8e-6, the
+// fit 2.2e-6.  A formula within 1.5e-7 of erf itself, which has no digit left at z = -6, measured 2.2 us less at 14,803 x 177 x 333 in fp32
+// (29.6, this 31.8) and 20 less at 118,417 x 512 x 2048 in bf16 (352, 372); the library's erff as much as this.
+template <bool FINE> __device__ __forceinline__ float gelu(float z) {
+  const float a = fabsf(z), s = a * a, t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.35f, a, 1.0f));      // (0 for a = inf, and then e^.. is too)
+  if (!FINE) {
+    constexpr float kF[] = {2.794835269e-01f, 2.748588622e-01f, 2.794893980e-01f, 3.817887977e-02f, 3.908216059e-01f, -3.448736966e-01f, 8.203927428e-02f};
+    const float p = horner(kF, t) * t * __builtin_amdgcn_exp2f(s * (-0.5f * kLog2e));
     return 0.5f * z * (z < 0.0f ? p : 2.0f - p);
   }
+  constexpr float kErf[] = {7.978845835e-01f, -1.329807192e-01f, 1.994664595e-02f, -2.372659976e-03f, 2.269727411e-04f, -1.530841655e-05f};
+  constexpr float kF[] = {-5.743541806e-06f, 2.794096172e-01f, 2.776412368e-01f, 2.542950809e-01f, 1.474193186e-01f,
+                          1.310321689e-01f, 1.578007825e-03f, -1.610362828e-01f, 6.988771260e-02f};
+  const float p = horner(kF, t) * exp_near(s, __builtin_fmaf(a, a, -s), -0.5f);
+  return 0.5f * z * (a < 1.0f ? 1.0f + z * horner(kErf, s) : z < 0.0f ? p : 2.0f - p);
+}
+
+// relu, silu and gelu as the header defines them; a NaN stays one
+template <bool FINE> __device__ __forceinline__ float activate(float z, int act) {
+  if (act == 1) return z < 0.0f ? 0.0f : z;
+  if (act == 2) return z * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));   // (the hardware's 1 / x is within 1 ulp)
+  if (act == 3) return gelu<FINE>(z);
   return z;
 }
 
@@ -86,18 +106,25 @@ __device__ __forceinline__ void store8(void *p, int64_t i, int dtype, int count,
   }
 }
 
+template <bool FINE> __device__ __forceinline__ void activate_all(int activation, float (&v)[8]) {
+  if (activation == 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = activate<FINE>(v[e], 1);
+  } else if (activation == 2) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = activate<FINE>(v[e], 2);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = activate<FINE>(v[e], 3);
+  }
+}
+
 // what follows the sums v (product and bias) of columns col.. of row m
 __device__ __forceinline__ void finish(const LinearArgs &a, int64_t m, int col, float (&v)[8]) {
   const int count = a.n - col;
-  if (a.activation == 1) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = activate(v[e], 1);
-  } else if (a.activation == 2) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = activate(v[e], 2);
-  } else if (a.activation == 3) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = activate(v[e], 3);
+  if (a.activation) {
+    if (a.out_dtype == 0) activate_all<true>(a.activation, v);
+    else activate_all<false>(a.activation, v);
   }
   if (a.scale != 1.0f) {
 #pragma unroll
