@@ -36,7 +36,7 @@ template <int N> __device__ __forceinline__ float horner(const float (&c)[N], fl
 // FINE, for fp32 results: within 8 (z < 0) and 2.5 (z > 0) times 2^-24 of itself, by an odd polynomial for erf below a = 1 (1 - F e^..
 // would lose digits near 0) and the exponent with what its square lost.  Else, for a result that is rounded to 16 bits: within 8e-6, the
 // fit 2.2e-6.  A formula within 1.5e-7 of erf itself, which has no digit left at z = -6, measured 2.2 us less at 14,803 x 177 x 333 in fp32
-// (29.6, this 31.8) and 20 less at 118,417 x 512 x 2048 in bf16 (352, 372); the library's erff as much as this.
+// (29.6, this 31.8) and 20 less at 118,417 x 512 x 2048 in bf16 (352, 372).
 template <bool FINE> __device__ __forceinline__ float gelu(float z) {
   const float a = fabsf(z), s = a * a, t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.35f, a, 1.0f));      // (0 for a = inf, and then e^.. is too)
   if (!FINE) {
@@ -51,10 +51,11 @@ template <bool FINE> __device__ __forceinline__ float gelu(float z) {
   return 0.5f * z * (a < 1.0f ? 1.0f + z * horner(kErf, s) : z < 0.0f ? p : 2.0f - p);
 }
 
-// relu, silu and gelu as the header defines them; a NaN stays one
+// relu, silu and gelu as the header defines them; a NaN stays one.  silu FINE is within 5 times 2^-24 of itself, else within 1.25 |z| 2^-24
+// more, where a 16-bit rounding is 2^13 of those.
 template <bool FINE> __device__ __forceinline__ float activate(float z, int act) {
   if (act == 1) return z < 0.0f ? 0.0f : z;
-  if (act == 2) return z * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));   // (the hardware's 1 / x is within 1 ulp)
+  if (act == 2) return FINE ? z / (1.0f + exp_near(-z)) : z * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));   // (1 / x of the hardware: 1 ulp)
   if (act == 3) return gelu<FINE>(z);
   return z;
 }

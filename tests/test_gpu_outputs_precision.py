@@ -50,3 +50,16 @@ def test_gelu_keeps_its_digits(m, n, out):
     got = through(z, n, "gelu", "f32").tolist()
     assert got[:2] == [0, 0] and got[4] == 1e4 and got[5] == 0 and got[7] == 0 and got[8] == math.inf and math.isnan(got[9])
     assert abs(got[2] / 1e-30 - 0.5) < 1e-6 and abs(got[3] / 1e-30 + 0.5) < 1e-6 and abs(got[6] / 3e38 - 1) < 1e-6
+
+
+@pytest.mark.parametrize("m,n", [(4001, 1), (40001, 1), (9001, 130)])
+@pytest.mark.parametrize("out", DT)
+def test_silu_keeps_its_digits(m, n, out):
+    """fp32: e^-z 3u (the hardware's 2^x, and what the exponent lost put back), the sum and the quotient u each.  16 bits: the exponent is off
+    by 1.25 u |z|, and 1 / x and a product come to it."""
+    z = torch.linspace(-80, 20, m, device="cuda")
+    relative(through(z, n, "silu", out), z.double() * torch.sigmoid(z.double()), 7 * U if out == "f32" else 128 * U, DT[out])
+    z = torch.tensor([0.0, -0.0, 1e-30, 1e4, -1e4, 3e38, -3e38, math.inf, math.nan, -88.5], device="cuda")
+    got = through(z, n, "silu", "f32").tolist()
+    assert got[:2] == [0, 0] and abs(got[2] / 5e-31 - 1) < 1e-6 and got[3] == 1e4 and got[4] == 0 and got[6] == 0 and got[7] == math.inf
+    assert abs(got[5] / 3e38 - 1) < 1e-6 and math.isnan(got[8]) and abs(got[9] / (-88.5 * math.exp(-88.5)) - 1) < 1e-5
