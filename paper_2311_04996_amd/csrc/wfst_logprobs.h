@@ -502,9 +502,27 @@ __global__ __launch_bounds__(kLongThreads) void logprobs_join_kernel(LogprobsArg
 
 // ---- the gradient
 struct Slope { float c, gh, h, m, ls; };                // of a row: p (c - gh (log p + h))
-__device__ __forceinline__ float grad_of(float x, Slope r) {
-  const float lp = (x - r.m) - r.ls;
-  return exp_fast(lp) * (r.c - r.gh * (fmaxf(lp, -1e4f) + r.h));
+// a - b and what it lost
+__device__ __forceinline__ float minus(float a, float b, float &lost) {
+  const float s = a - b, t = s - a;
+  lost = (a - (s - t)) - (b + t);
+  return s;
+}
+// For fp32 scores p has all its digits however small it is: the roundings of log p are kept (within 3 times 2^-24 of itself; without
+// that 125 times at log p = -80).  It costs 2 us of 27 at 118,417 rows of 129 and nothing at 2,048 of 64,001 (202 us).  For 16-bit scores the
+// result's own rounding is 2^13 to 2^16 of those.
+template <class E> __device__ __forceinline__ float grad_of(float x, Slope r) {
+  float lp, p;
+  if constexpr (sizeof(typename E::T) == 4) {
+    float lost_m, lost_ls;
+    const float d = minus(x, r.m, lost_m);
+    lp = minus(d, r.ls, lost_ls);
+    p = exp_near(lp, lost_m + lost_ls);
+  } else {
+    lp = (x - r.m) - r.ls;
+    p = exp_fast(lp);
+  }
+  return p * (r.c - r.gh * (fmaxf(lp, -1e4f) + r.h));
 }
 // Token i of the given and the top ones, and its gradient; -1 if it has none.
 __device__ __forceinline__ int named(const BackwardArgs &a, int64_t row, int i, float &g) {
@@ -548,7 +566,7 @@ __global__ __launch_bounds__(256) void backward_short_kernel(BackwardArgs a) {
   const bool empty = is_empty(r.m, r.ls);
 #pragma unroll
   for (int e = 0; e < EACH; ++e)
-    if (lane + LANES * e < a.v) dx[lane + LANES * e] = E::put(empty ? 0.0f : grad_of(z[e], r) + extra[e]);
+    if (lane + LANES * e < a.v) dx[lane + LANES * e] = E::put(empty ? 0.0f : grad_of<E>(z[e], r) + extra[e]);
 }
 
 // A workgroup per part of a long row.  Scores that a token names are read first (the gradient may take the scores' place) and
@@ -599,7 +617,7 @@ __global__ __launch_bounds__(kLongThreads) void backward_long_kernel(BackwardArg
     if (where[k] < 0) continue;
     float extra = 0.0f;
     for (int f = i; f < n; ++f) extra += ids[f] == j ? grads[f] : 0.0f;
-    late[k] = empty ? 0.0f : grad_of(E::get(x[j]), r) + extra;
+    late[k] = empty ? 0.0f : grad_of<E>(E::get(x[j]), r) + extra;
   }
   __syncthreads();                                     // the named scores have been read
 #pragma unroll
@@ -607,7 +625,7 @@ __global__ __launch_bounds__(kLongThreads) void backward_long_kernel(BackwardArg
     const int64_t j = lo + tid * C::kN + i * kStep;
     typename C::Vec d;
 #pragma unroll
-    for (int e = 0; e < C::kN; ++e) d[e] = E::put(empty ? 0.0f : grad_of(E::get(c[i][e]), r));
+    for (int e = 0; e < C::kN; ++e) d[e] = E::put(empty ? 0.0f : grad_of<E>(E::get(c[i][e]), r));
     if (j + C::kN <= hi) {
       C::store(dx + j, d);
     } else {

@@ -11,7 +11,7 @@ torch = pytest.importorskip("torch")
 if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
-from paper_2311_04996_amd import linear  # noqa: E402
+from paper_2311_04996_amd import linear, token_logprobs, token_logprobs_backward  # noqa: E402
 
 U = 2.0 ** -24
 DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
@@ -63,3 +63,18 @@ def test_silu_keeps_its_digits(m, n, out):
     got = through(z, n, "silu", "f32").tolist()
     assert got[:2] == [0, 0] and abs(got[2] / 5e-31 - 1) < 1e-6 and got[3] == 1e4 and got[4] == 0 and got[6] == 0 and got[7] == math.inf
     assert abs(got[5] / 3e38 - 1) < 1e-6 and math.isnan(got[8]) and abs(got[9] / (-88.5 * math.exp(-88.5)) - 1) < 1e-5
+
+
+@pytest.mark.parametrize("v", [29, 129, 500, 2048, 2049, 40001])
+def test_the_gradient_keeps_the_digits_of_small_probabilities(v):
+    """The gradient of lse is p itself, e^(x - maximum - log_sum) of the forward call's maximum and log_sum.  The roundings of the two
+    differences are kept: the hardware's 2^x 2u, what is put back u, the product with the slope of 1 nothing: 3u, and 2^-24 of
+    the roundings themselves."""
+    g = torch.Generator(device="cuda").manual_seed(v)
+    x = torch.randn((50, v), generator=g, device="cuda") * 6
+    x[:, 0] = torch.linspace(-60, 0, 50, device="cuda")
+    r = token_logprobs(x)
+    want = torch.exp((x.double() - r.maximum.double()[:, None]) - r.log_sum.double()[:, None])
+    got = token_logprobs_backward(x, r, grad_lse=torch.ones(50, device="cuda"))
+    assert float(want.min()) >= 2.0 ** -126                                        # (all of them normal numbers)
+    relative(got, want, 5 * U)
