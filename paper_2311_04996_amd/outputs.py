@@ -31,13 +31,14 @@ torch = lib = _codes = _raw_stream = None
 
 
 def _start():
-    """On the first call: the library, and torch with it."""
+    """On the first call: the library, and torch with it.  `lib` comes last: another thread takes it as the sign that all is there."""
     global torch, lib, _codes, _raw_stream
-    lib = load_library()
+    library = load_library()
     import torch as t
     _codes = {t.float32: 0, t.float16: 1, t.bfloat16: 2}
     _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda dev: t.cuda.current_stream(dev).cuda_stream)
     torch = t
+    lib = library
 
 
 def _device(t, what):
