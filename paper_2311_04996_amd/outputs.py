@@ -20,9 +20,10 @@ ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 
 def _packer(args):
-    """The argument struct as bytes, in one step (filling a ctypes struct costs a small call a tenth of its time)."""
+    """The argument struct as bytes, in one step (filling a ctypes struct costs a small call a tenth of its time).  "0P": all of
+    it, up to the next multiple of a pointer, as the library may copy it whole."""
     letter = {C.c_void_p: "P", C.c_int64: "q", C.c_int32: "i", C.c_float: "f"}
-    return struct.Struct("@" + "".join(letter[t] for _, t in args._fields_))
+    return struct.Struct("@" + "".join(letter[t] for _, t in args._fields_) + "0P")
 
 
 _linear, _loglikes = _packer(wfst_linear_args), _packer(wfst_loglikes_args)

@@ -1,10 +1,11 @@
-"""The host side of the operators beside the decoder, without a GPU: first calls from several threads."""
+"""The host side of the operators beside the decoder, without a GPU: first calls from several threads, the arguments as bytes."""
+import ctypes as C
 import os
 import sys
 
 import pytest
 
-from paper_2311_04996_amd import LIB_PATH, build_library, outputs
+from paper_2311_04996_amd import LIB_PATH, binding, build_library, outputs
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -33,3 +34,9 @@ def test_the_library_is_there_only_when_all_of_it_is(monkeypatch):
     finally:
         sys.settrace(before)
     assert early == [] and outputs.lib is not None and outputs.torch is not None
+
+
+@pytest.mark.parametrize("entry", ["linear", "loglikes", "token_logprobs", "token_logprobs_backward"])
+def test_packed_arguments_are_a_whole_struct(entry):
+    """The library is handed all of the struct, the padding behind its last field too."""
+    assert outputs._packer(getattr(binding, f"wfst_{entry}_args")).size == C.sizeof(getattr(binding, f"wfst_{entry}_args"))
