@@ -10,8 +10,9 @@
  * Conventions
  *   - Every call returns a status (0 = WFST_OK, negative = error).  Nothing throws or aborts
  *     across this boundary.  wfst_last_error() gives a library-owned message for the last
- *     failing call on that decoder (when passed NULL: for the calling thread's last failing creation
- *     or call that takes no decoder).
+ *     failing call on that decoder.  When passed NULL: for the process's last failing creation, on
+ *     whichever thread, or, if it came later or has not been asked for yet, the calling thread's own last failing
+ *     call that takes no decoder.  (That message stays until the thread asks again or ends.)
  *   - "host" / "device" on a pointer says where the memory lives.  The library never takes
  *     ownership of caller memory; graph arrays are copied during create.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Work is

@@ -2357,7 +2357,23 @@ struct wfst_decoder {
 };
 
 namespace {
-thread_local std::string g_create_err;    // of creations and of calls without a decoder
+// What wfst_last_error(NULL) answers: the process's last failing creation, whichever thread made it, or the thread's own last
+// failing call that takes no decoder.  The later one counts, but another thread's creation does not take the place of such a call's
+// message before that was read; and after such a call a creation's message is its own thread's only.
+struct Note { std::string msg; uint64_t at = 0; };         // the at-th of the process, 0: none
+std::mutex g_notes_lock;
+Note g_creation;
+uint64_t g_notes = 0;
+thread_local Note t_note;
+thread_local bool t_unread = false;
+
+void note_creation(const std::string &msg) {
+  const std::lock_guard<std::mutex> lock(g_notes_lock);
+  g_creation.msg = msg;
+  g_creation.at = ++g_notes;
+  t_note = g_creation;
+  t_unread = false;
+}
 
 #define HIP_TRY(dec, expr)                                                              \
   do {                                                                                  \
@@ -2384,7 +2400,7 @@ template <class T> int dev_alloc(wfst_decoder *d, T **p, size_t n) {
 }
 
 int fail(wfst_decoder *d, int code, const std::string &msg) {
-  if (d) d->err = msg; else g_create_err = msg;
+  if (d) d->err = msg; else note_creation(msg);
   return code;
 }
 
@@ -3234,7 +3250,7 @@ int32_t wfst_decoder_create(const wfst_graph_csr *graph, const wfst_opts *opts, 
     if (hipEventCreate(&d->ev0[i]) != hipSuccess || hipEventCreate(&d->ev1[i]) != hipSuccess) {
       d->err = "hipEventCreate failed"; rc = WFST_ERR_HIP;
     }
-  if (rc) { g_create_err = d->err; wfst_decoder_destroy(d); return rc; }
+  if (rc) { note_creation(d->err); wfst_decoder_destroy(d); return rc; }
   {
     // learn this device's address of the static scratch now rather than in the first call that needs it
     unsigned long long *p = nullptr;
@@ -3707,11 +3723,26 @@ float wfst_slot_kernel_ms(wfst_decoder *d, int32_t slot) {
   return ms;
 }
 
-const char *wfst_last_error(const wfst_decoder *d) { return d ? d->err.c_str() : g_create_err.c_str(); }
+const char *wfst_last_error(const wfst_decoder *d) {
+  if (d) return d->err.c_str();
+  try {
+    const std::lock_guard<std::mutex> lock(g_notes_lock);
+    if (!t_unread && g_creation.at > t_note.at) t_note = g_creation;
+    t_unread = false;
+    return t_note.msg.c_str();
+  } catch (...) { return ""; }                             // (no memory for the copy)
+}
 
 }  // extern "C"
 
 int wfst_note_error(int code, const char *msg) noexcept {
-  try { g_create_err = msg; } catch (...) { g_create_err.clear(); }
+  try {
+    const std::lock_guard<std::mutex> lock(g_notes_lock);
+    t_note.at = ++g_notes;
+    t_note.msg.clear();
+    t_unread = true;
+    g_creation.at = 0;
+    t_note.msg = msg;
+  } catch (...) {}
   return code;
 }

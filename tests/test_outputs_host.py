@@ -1,7 +1,9 @@
-"""The host side of the operators beside the decoder, without a GPU: first calls from several threads, the arguments as bytes."""
+"""The host side of the operators beside the decoder, without a GPU: first calls from several threads, the arguments as
+bytes, the messages of failing calls."""
 import ctypes as C
 import os
 import sys
+import threading
 
 import pytest
 
@@ -40,3 +42,32 @@ def test_the_library_is_there_only_when_all_of_it_is(monkeypatch):
 def test_packed_arguments_are_a_whole_struct(entry):
     """The library is handed all of the struct, the padding behind its last field too."""
     assert outputs._packer(getattr(binding, f"wfst_{entry}_args")).size == C.sizeof(getattr(binding, f"wfst_{entry}_args"))
+
+
+def elsewhere(call):
+    """What `call` returns on a thread of its own."""
+    got = []
+    t = threading.Thread(target=lambda: got.append(call()))
+    t.start()
+    t.join()
+    return got[0]
+
+
+def test_a_failing_creation_is_told_on_any_thread():
+    lib = binding.load_library()
+    message = lambda: lib.wfst_last_error(None).decode()
+    graph, opts, handle = binding.wfst_graph_csr(), binding.wfst_opts(), C.c_void_p()
+    create = lambda: lib.wfst_decoder_create(C.byref(graph), C.byref(opts), C.byref(handle))      # all of them 0: refused before any GPU call
+    refuse = lambda: lib.wfst_linear(C.byref(binding.wfst_linear_args()), None)
+
+    assert elsewhere(create) == -1
+    assert "max_channels" in message() and "max_channels" in message() and "max_channels" in elsewhere(message)
+    # a call without a decoder: on its own thread only, and what a creation of another thread says does not come before it is read
+    assert refuse() == -1 and elsewhere(message) == ""
+    opts.max_channels = opts.max_frames_per_channel = opts.max_words = 1
+    opts.loglike_dtype = 9
+    assert elsewhere(create) == -1
+    assert message().startswith("wfst_linear:") and "loglike_dtype" in message() and "loglike_dtype" in elsewhere(message)
+    # a creation's own thread keeps its message, whatever fails elsewhere
+    assert create() == -1 and elsewhere(refuse) == -1
+    assert "loglike_dtype" in message() and elsewhere(message) == ""
