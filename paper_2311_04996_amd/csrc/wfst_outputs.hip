@@ -63,8 +63,8 @@ bool rows_apart(int64_t seqs, int64_t frames, int64_t cols, int64_t seq_stride, 
 }
 
 // Every row starts at a multiple of 16 bytes and is a whole number of 16-byte chunks, and the 256 rows of a tile are within 2 GB.
-bool chunked(const void *p, int64_t rows, int64_t stride, int64_t k, int64_t size) {
-  return aligned(p, 16) && k * size % 16 == 0 && (rows == 1 || (stride * size % 16 == 0 && stride < ((1 << 30) - k) / size / 128));
+bool chunked(const void *p, int64_t stride, int64_t k, int64_t size) {
+  return aligned(p, 16) && k * size % 16 == 0 && stride * size % 16 == 0 && stride < ((1 << 30) - k) / size / 128;
 }
 
 template <class F> int by_type(int32_t dtype, F f) { return dtype == 0 ? f(F32{}) : dtype == 1 ? f(F16{}) : f(BF16{}); }
@@ -215,9 +215,11 @@ int32_t wfst_linear(const wfst_linear_args *args, void *stream) {
     return refuse(me, "y overlaps what is read");
   if (overlap(p.y, ny, p.residual, nr) && !(p.residual == p.y && (p.residual_stride == p.y_stride || p.rows == 1)))
     return refuse(me, "y overlaps the residual without being it");
-  LinearArgs a{p.x, p.w, p.bias, p.residual, p.y, p.rows, p.x_stride, p.w_stride, p.residual_stride, p.y_stride,
+  // The stride of a single row is no one's promise: behind it a tile reads that row again, not what lies a stride further on.
+  const int64_t x_stride = p.rows == 1 ? 0 : p.x_stride, w_stride = p.n == 1 ? 0 : p.w_stride;
+  LinearArgs a{p.x, p.w, p.bias, p.residual, p.y, p.rows, x_stride, w_stride, p.residual_stride, p.y_stride,
                p.k, p.n, p.bias_dtype, p.out_dtype, p.activation, p.scale, 0};
-  const bool direct = chunked(p.x, p.rows, p.x_stride, p.k, size) && chunked(p.w, p.n, p.w_stride, p.k, size);
+  const bool direct = chunked(p.x, x_stride, p.k, size) && chunked(p.w, w_stride, p.k, size);
   return by_type(p.dtype, [&](auto e) { return run_linear<decltype(e)>(a, direct, stream); });
 }
 
