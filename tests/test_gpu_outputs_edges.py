@@ -12,7 +12,7 @@ if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
 from paper_2311_04996_amd import linear  # noqa: E402
-from test_gpu_outputs import DT, check_linear, gen, randn  # noqa: E402
+from test_gpu_outputs import DT, U, act64, check_linear, close, gen, randn, round_off, wide  # noqa: E402
 
 
 @pytest.mark.parametrize("dt", DT)
@@ -25,3 +25,73 @@ def test_linear_of_one_row_whatever_its_stride(stride, dt):
     flat = randn(g, k + 8).to(DT[dt])
     check_linear(one(flat[:k]), (randn(g, 4200, k) / 8).to(DT[dt]), randn(g, 4200), "silu")
     check_linear(randn(g, 4200, k).to(DT[dt]), one(flat[8:]), randn(g, 1), "relu")
+
+
+# ------------------------------------------------------------------------------------- every tile of wfst_linear
+def tiles(m, n, bm, bn):
+    return -(-m // bm) * -(-n // bn)
+
+
+def chosen(dt, m, n, direct):
+    """The tile that a product gets, as the library's rule says."""
+    if tiles(m, n, 16, 16) <= 256:
+        return "16x16"
+    if dt == "f32":
+        t = tiles(m, n, 128, 128)
+        return "128x128" if t >= 256 and t * 8 >= -(-t // 256) * 256 * 7 else "64x64"
+    if direct and tiles(m, n, 256, 256) >= 256:
+        return "256x256"
+    if tiles(m, n, 256, 128) >= 256:
+        return "256x128"
+    if tiles(m, n, 128, 128) >= 256:
+        return "128x128"
+    return "32x64" if direct and tiles(m, n, 32, 64) <= 256 else "64x64"
+
+
+def check_on_gpu(x, w, b, act, r, scale, out, out_dtype):
+    """check_linear with the 64-bit side on the GPU; x, w, r may be views of wider buffers, out the left part of one."""
+    xd, wd = x.double().contiguous(), w.double().t().contiguous()
+    z, mag = torch.matmul(xd, wd), torch.matmul(xd.abs(), wd.abs())
+    if b is not None:
+        z, mag = z + b.double(), mag + b.double().abs()
+    a, tol = act64(z, act), 1.13 * (x.shape[1] + 8) * 2 * U * mag
+    if act in ("silu", "gelu"):
+        tol = tol + (z.abs() + 4) * 8 * U * torch.maximum(a.abs(), torch.full_like(a, 0.25))
+    want, tol = scale * a, abs(scale) * tol + 4 * U * (scale * a).abs()
+    if r is not None:
+        want = want + r.double()
+    got = linear(x, w, b, activation=act, residual=r, scale=scale, out=out, out_dtype=out_dtype)
+    close(got, want, tol + 4 * U * want.abs() + round_off(want, got.dtype))
+
+
+# rows, columns, tile of whole chunks, tile of other rows.  Each just past the size from which there are 256 of its tiles, with a rest in
+# both directions (and the largest ones with a row and a column that is alone in its tile).
+TILES = [("f16", 8193, 2049, "256x256", "256x128"), ("bf16", 8193, 2049, "256x256", "256x128"), ("bf16", 4081, 4010, "256x256", "256x128"),
+         ("f16", 4097, 2049, "256x128", "256x128"), ("bf16", 4000, 2050, "256x128", "256x128"),
+         ("f16", 4097, 1025, "128x128", "128x128"), ("bf16", 2100, 2030, "128x128", "128x128"),
+         ("f32", 3969, 1000, "128x128", "128x128"), ("f32", 7601, 1021, "128x128", "128x128"), ("f32", 4097, 1025, "64x64", "64x64"),
+         ("f16", 1001, 500, "32x64", "64x64"), ("bf16", 1200, 700, "64x64", "64x64"), ("f32", 1200, 700, "64x64", "64x64")]
+
+
+@pytest.mark.parametrize("direct", [True, False])
+@pytest.mark.parametrize("dt,m,n,whole,other", TILES)
+def test_linear_in_every_tile(dt, m, n, whole, other, direct):
+    """Less than a part of k (64 or 128 bytes), and so many parts that a turn of three or four stages ends in each of its places."""
+    assert chosen(dt, m, n, direct) == (whole if direct else other)
+    g = gen(m, n, direct)
+    chunk = 128 // torch.finfo(DT[dt]).bits                                        # elements of 16 bytes
+    for i, chunks in enumerate((1, 6, 9, 13, 17, 23, 32)):
+        k = chunks * chunk if direct else chunks * chunk - 1 - i % (chunk - 1)
+        act, scale = (None, "relu", "silu", "gelu")[i % 4], (1.0, 0.5, -2.0)[i % 3]
+        x, w = randn(g, m, k).to(DT[dt]), (randn(g, n, k) / math.sqrt(k)).to(DT[dt])
+        out = None
+        out_dtype = DT[("f32", "f16", "bf16")[i % 3]]
+        r = randn(g, m, n).to(out_dtype) if i % 2 else None
+        if i % 3 == 1:                                                             # NaN between the rows, results in a wider buffer
+            pad = 8 if direct else 3
+            x, w, r = wide(x, pad), wide(w, pad), None if r is None else wide(r, pad)
+            whole_out = torch.full((m, n + 5), 7.0, dtype=out_dtype, device="cuda")
+            out = whole_out[:, :n]
+        check_on_gpu(x, w, randn(g, n) if i else None, act, r, scale, out, out_dtype)
+        if out is not None:
+            assert bool((whole_out[:, n:] == 7.0).all())
