@@ -11,8 +11,9 @@ torch = pytest.importorskip("torch")
 if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
-from paper_2311_04996_amd import linear  # noqa: E402
-from test_gpu_outputs import DT, U, act64, check_linear, close, gen, randn, round_off, wide  # noqa: E402
+from paper_2311_04996_amd import linear, loglikes, token_logprobs, token_logprobs_backward  # noqa: E402
+from test_gpu_outputs import DT, U, act64, backward64, check_backward, check_linear, check_logprobs, check_loglikes, close, gen, randn, \
+    round_off, wide  # noqa: E402
 
 
 @pytest.mark.parametrize("dt", DT)
@@ -95,3 +96,52 @@ def test_linear_in_every_tile(dt, m, n, whole, other, direct):
         check_on_gpu(x, w, randn(g, n) if i else None, act, r, scale, out, out_dtype)
         if out is not None:
             assert bool((whole_out[:, n:] == 7.0).all())
+
+
+# ------------------------------------------------------------------- wfst_loglikes about where its tiles change
+@pytest.mark.parametrize("k", [72, 200, 35])
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("v", [160, 161, 256, 257, 512, 513, 1024, 1025, 1152, 1153, 1536, 1537, 2048])
+def test_loglikes_about_the_sizes_where_tiles_change(v, dt, k):
+    """Right in the largest call, and the same bits in those that other tiles compute."""
+    g = gen(v, k, 3)
+    x, w, b = randn(g, 8193, k).to(DT[dt]), (randn(g, v, k) * 2 / math.sqrt(k)).to(DT[dt]), randn(g, v)
+    whole = loglikes(x, w, b)
+    rows = [0, 1, 31, 32, 63, 64, 127, 128, 4095, 4096, 8191, 8192, *range(200, 8000, 397)]      # of every place in a tile
+    check_loglikes(x[rows], w, b)
+    assert torch.equal(loglikes(x[rows], w, b), whole[rows])
+    for n in (4096, 4097, 8192):
+        assert torch.equal(loglikes(x[:n], w, b), whole[:n])
+    lengths = torch.tensor([2731, 0, 2000], dtype=torch.int32, device="cuda")
+    x3 = x.view(3, 2731, k)
+    got = loglikes(x3, w, b, lengths=lengths, out=torch.full((3, 2731, v), 4.0, device="cuda"))
+    assert torch.equal(got[0], whole[:2731]) and torch.equal(got[2, :2000], whole[5462:7462])
+    assert bool((got[1] == 4.0).all() and (got[2, 2000:] == 4.0).all())
+
+
+# ------------------------------------------------------------------- as many named tokens as there may be
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("v", [64, 129, 300, 2048, 2049, 9000, 70001])
+def test_as_many_tokens_as_there_may_be(v, dt):
+    """255, 256 and the 64 best ones: behind the 256th a thread of the long rows has two of them.  All different ones, the same one always, and
+    some of both; given ones that are the best ones too; next to a limit of what one workgroup has of a row."""
+    g = gen(v, 99)
+    for given, top in ((256, 64), (255, 64), (256, 0), (192, 64), (193, 64)):
+        x = (randn(g, 6, v) * 3).to(DT[dt])
+        tokens = torch.stack([torch.randperm(max(v, given), generator=g, device="cuda")[:given] for _ in range(6)]).int()
+        tokens[tokens >= v] = -1
+        tokens[1] = v - 1
+        tokens[2, 100:] = 3
+        best = torch.topk(x[3].float(), 64).indices.int()
+        tokens[3, given - 64:] = best
+        tokens[4, ::2] = -1
+        tokens[5] = torch.arange(given, device="cuda") % 9
+        check_logprobs(x, tokens, top)
+        check_backward(x, tokens, top, g)
+        check_backward(x, tokens, top, g, lse=False, ent=False)
+    y = x.clone()                                                                  # over the scores themselves
+    r = token_logprobs(x, tokens, top=64)
+    gl, gt = randn(g, 6, given), randn(g, 6, 64)
+    want, tol = backward64(x, tokens, r.top_ids, gl, None, None, gt)
+    got = token_logprobs_backward(y, r, tokens, grad_logprobs=gl, grad_top=gt, out=y)
+    close(got, want, tol + round_off(want, DT[dt]))
