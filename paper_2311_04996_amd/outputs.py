@@ -3,9 +3,10 @@ states, and the probabilities of what was decoded.
 
 Argument marshalling only, like `binding`: every function enqueues HIP kernels on `stream` (default: torch's current
 stream of the tensors' device) and returns without waiting.  All tensors of a call are on one GPU, which need not be the
-current one.  Results are new tensors (allocated on `stream`) unless `out` gives them.  Nothing is recorded by
-autograd: `token_logprobs` has its gradient as a function of its own.  Shapes, types and layouts that a kernel does not
-take raise ValueError here, what else is wrong with a call raises WfstError.
+current one.  Results are new tensors (allocated on `stream`) unless `out` gives them.  `linear` and `loglikes` are
+for serving: they have no gradient, and their results are detached.  `token_logprobs` is recorded by autograd where
+its scores require a gradient, and has its gradient as a function of its own, too.  Shapes, types and layouts that a kernel
+does not take raise ValueError here, what else is wrong with a call raises WfstError.
 """
 from __future__ import annotations
 
@@ -28,16 +29,43 @@ def _packer(args):
 
 _linear, _loglikes = _packer(wfst_linear_args), _packer(wfst_loglikes_args)
 _logprobs, _backward = _packer(wfst_token_logprobs_args), _packer(wfst_token_logprobs_backward_args)
-torch = lib = _codes = _raw_stream = None
+torch = lib = _codes = _raw_stream = _Recorded = None
+
+
+def _recorded(torch):
+    """The autograd function of `token_logprobs` (torch is not imported before the first call)."""
+    from torch.autograd.function import once_differentiable
+
+    class TokenLogprobsFunction(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, scores, tokens, top, lengths, stream):
+            r = _token_logprobs(scores, tokens, top, lengths, stream)
+            ctx.save_for_backward(scores, tokens, lengths, r.entropy, r.maximum, r.log_sum, r.top_ids)
+            ctx.mark_non_differentiable(*(t for t in (r.maximum, r.log_sum, r.top_ids) if t is not None))
+            ctx.set_materialize_grads(False)
+            return tuple(r)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, grad_logprobs, grad_lse, grad_entropy, grad_maximum, grad_log_sum, grad_ids, grad_top):
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("token_logprobs: autograd's backward pass is not recorded into a graph: call token_logprobs_backward there")
+            scores, tokens, lengths, entropy, maximum, log_sum, top_ids = ctx.saved_tensors
+            result = TokenLogprobs(None, None, entropy, maximum, log_sum, top_ids, None)
+            g_lp, g_lse, g_h, g_top = (None if g is None else g.contiguous() for g in (grad_logprobs, grad_lse, grad_entropy, grad_top))
+            return token_logprobs_backward(scores, result, tokens, g_lp, g_lse, g_h, g_top, lengths=lengths), None, None, None, None
+
+    return TokenLogprobsFunction
 
 
 def _start():
     """On the first call: the library, and torch with it.  `lib` comes last: another thread takes it as the sign that all is there."""
-    global torch, lib, _codes, _raw_stream
+    global torch, lib, _codes, _raw_stream, _Recorded
     library = load_library()
     import torch as t
     _codes = {t.float32: 0, t.float16: 1, t.bfloat16: 2}
     _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda dev: t.cuda.current_stream(dev).cuda_stream)
+    _Recorded = _recorded(t)
     torch = t
     lib = library
 
@@ -138,7 +166,7 @@ def _run(entry, args, dev, stream):
 
 
 def linear(x, weight, bias=None, activation=None, residual=None, scale=1.0, out=None, out_dtype=None, stream=None):
-    """residual + scale * activation(x @ weight.T + bias), in one kernel (wfst_linear).
+    """residual + scale * activation(x @ weight.T + bias), in one kernel (wfst_linear).  No gradient: the result is detached.
 
     x: [..., k] and weight: [n, k], of one type (float32, float16 or bfloat16); their rows may have any stride.
     bias: [n], any of the types.  activation: None, "relu", "silu" or "gelu" (with erf).  residual: [..., n] of the
@@ -181,7 +209,7 @@ def linear(x, weight, bias=None, activation=None, residual=None, scale=1.0, out=
 
 def loglikes(hidden, weight, bias=None, log_prior=None, lengths=None, out=None, out_dtype=None, stream=None):
     """log_softmax(hidden @ weight.T + bias) - log_prior, in one kernel (wfst_loglikes): what `Decoder.decode_batch` and
-    `Decoder.advance_chunk` take.
+    `Decoder.advance_chunk` take.  No gradient: the result is detached.
 
     hidden: [frames, k] or [sequences, frames, k], any strides of its first dimensions (time-major hidden states are
     given transposed); weight: [v, k] of hidden's type, v <= 2048; bias: [v]; log_prior: float32 [v].
@@ -230,8 +258,22 @@ def token_logprobs(scores, tokens=None, top=0, lengths=None, stream=None):
     scores: [rows, v] or [sequences, frames, v] logits or log-likelihoods, float32, float16 or bfloat16, any strides of
     the first dimensions.  tokens: int32 [..., given] (or [...], one per row), -1 for none; at most 256 per row.  top: 0 to 64.
     lengths: int32 CUDA tensor [sequences]: rows behind a sequence's length are not read, their results are 0.
-    A row that rules everything out (-inf) has lse -inf, log-probabilities -inf and entropy 0."""
-    dev = _device(scores, "scores")
+    A row that rules everything out (-inf) has lse -inf, log-probabilities -inf and entropy 0.
+
+    Where the scores require a gradient (and grad mode is on) autograd records the call: logprobs, lse, entropy and top_logprobs have
+    the gradient that token_logprobs_backward computes, the others are constants.  Its backward pass is not for graphs under capture
+    (RuntimeError): there, token_logprobs_backward is called itself."""
+    _device(scores, "scores")
+    if not (scores.requires_grad and torch.is_grad_enabled()):
+        return _token_logprobs(scores, tokens, top, lengths, stream)
+    if stream is None:
+        return TokenLogprobs(*_Recorded.apply(scores, tokens, top, lengths, None))
+    with torch.cuda.stream(stream):                      # (autograd runs the backward pass on the forward's current stream)
+        return TokenLogprobs(*_Recorded.apply(scores, tokens, top, lengths, stream))
+
+
+def _token_logprobs(scores, tokens, top, lengths, stream):
+    dev = scores.get_device()
     code = _code(scores, "scores")
     seqs, frames, ss, st = _grid(scores, "scores")
     lead, v = scores.shape[:-1], scores.shape[-1]
@@ -249,7 +291,10 @@ def token_logprobs(scores, tokens=None, top=0, lengths=None, stream=None):
         tok = _dense(tokens, shape, i32, "tokens", dev)
         lp = _new(new, shape, f32, on, stream)
         lp_at = lp.data_ptr()
-    lse, entropy, maximum, log_sum = _new(new, (4, *lead), f32, on, stream).unbind(0)
+    if scores.requires_grad:                             # (autograd wants results that are no views)
+        lse, entropy, maximum, log_sum = (_new(new, lead, f32, on, stream) for _ in range(4))
+    else:
+        lse, entropy, maximum, log_sum = _new(new, (4, *lead), f32, on, stream).unbind(0)
     if top > 0:
         ids, tlp = _new(new, (*lead, top), i32, on, stream), _new(new, (*lead, top), f32, on, stream)
         ids_at, tlp_at = ids.data_ptr(), tlp.data_ptr()
