@@ -426,6 +426,9 @@ class Decoder:
         from .outputs import loglikes as output_layer
         if hidden.dim() != 3 or weight.shape[0] != self.V:
             raise ValueError(f"hidden {tuple(hidden.shape)} must have three dimensions and weight {tuple(weight.shape)} {self.V} rows")
+        if stream is None and hidden.is_cuda and hidden.get_device() != torch.cuda.current_device():
+            # the output layer would run on a stream of that GPU and the decoder, without waiting for it, on one of the current GPU
+            raise ValueError(f"hidden is on {hidden.device}: the decoder's GPU must be the current one, or its stream given")
         if len(lengths) != hidden.shape[0] or (len(lengths) and not (0 <= lengths.min() and lengths.max() <= hidden.shape[1])):
             raise ValueError("lengths must have an entry between 0 and the number of frames for every row of hidden")
         with _on(stream):

@@ -1,5 +1,6 @@
 """The host side of the operators beside the decoder, without a GPU: first calls from several threads, the arguments as
-bytes, the messages of failing calls."""
+bytes, the messages of failing calls, hidden states on
+another GPU."""
 import ctypes as C
 import os
 import sys
@@ -71,3 +72,21 @@ def test_a_failing_creation_is_told_on_any_thread():
     # a creation's own thread keeps its message, whatever fails elsewhere
     assert create() == -1 and elsewhere(refuse) == -1
     assert "loglike_dtype" in message() and elsewhere(message) == ""
+
+
+def test_hidden_states_on_another_gpu_than_the_current_one_are_refused(monkeypatch):
+    """The decoder runs on the current GPU's stream, which does not wait for one of another GPU."""
+    import torch
+    decoder = object.__new__(binding.Decoder)
+    decoder.V, decoder.loglike_dtype = 29, "float32"
+
+    class Elsewhere:                                       # a tensor on cuda:1
+        is_cuda, shape, device = True, (2, 5, 8), "cuda:1"
+        dim = staticmethod(lambda: 3)
+        get_device = staticmethod(lambda: 1)
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    for call in (lambda: decoder.decode_hidden(Elsewhere(), [5, 5], torch.zeros(29, 8), None, 10.0, 100),
+                 lambda: decoder.advance_hidden_partial([0, 1], Elsewhere(), [5, 5], torch.zeros(29, 8), None)):
+        with pytest.raises(ValueError, match="cuda:1"):
+            call()
