@@ -449,7 +449,7 @@ class Decoder:
         """decode_batch of loglikes(hidden, weight, bias, log_prior): hidden: CUDA tensor [B, T, k] of an encoder (any
         strides of B and T); weight [V, k], bias [V] or None: its output layer; lengths: int32 host array [B].
         loglikes: a contiguous [B, T, V] tensor of the decoder's type to keep them in (get_lattice needs them); only frames
-        before a length are written.  Other arguments and the results as in decode_batch."""
+        before a length are written, less log_prior if that is given.  Other arguments and the results as in decode_batch."""
         lengths = np.ascontiguousarray(lengths, dtype=np.int32)
         ll = self._loglikes(hidden, weight, bias, log_prior, lengths, loglikes, stream)
         return self.decode_batch(ll, lengths, beam, max_active, stream=stream, **kw)

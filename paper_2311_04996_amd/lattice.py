@@ -101,8 +101,10 @@ class Lattice:
 
     def path_logprobs(self, scores, paths, top=0, stream=None):
         """How sure the model was of the labels of n paths, frame by frame: token_logprobs of scores (CUDA [num_frames,
-        V], the model's logits or log-likelihoods) at the paths' labels: logprobs [num_frames, n], and of every frame lse,
-        entropy and the `top` best labels.  paths: at most 256 lists of link indices, as nbest gives them."""
+        V], the model's logits or log-probabilities) at the paths' labels: logprobs [num_frames, n], and of every frame lse,
+        entropy and the `top` best labels.  paths: at most 256 lists of link indices, as nbest gives them.
+        Rows that were decoded with log priors taken off (loglikes and decode_hidden with log_prior) are no probabilities,
+        and their softmax is not the model's: give rows + log_prior."""
         import torch
         from .binding import _on
         from .outputs import token_logprobs

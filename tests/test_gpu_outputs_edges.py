@@ -145,3 +145,17 @@ def test_as_many_tokens_as_there_may_be(v, dt):
     want, tol = backward64(x, tokens, r.top_ids, gl, None, None, gt)
     got = token_logprobs_backward(y, r, tokens, grad_logprobs=gl, grad_top=gt, out=y)
     close(got, want, tol + round_off(want, DT[dt]))
+
+
+def test_confidence_of_rows_that_had_the_priors_taken_off():
+    """What Lattice.path_logprobs asks for: rows + log_prior have the model's probabilities again, the rows alone have not."""
+    g = gen(300)
+    x, w, b = randn(g, 40, 64), randn(g, 29, 64) / 4, randn(g, 29)
+    prior = torch.log_softmax(randn(g, 29) * 2, 0)
+    tokens = (torch.arange(40, device="cuda") % 29).int()[:, None]
+    want = loglikes(x, w, b).gather(1, tokens.long())
+    rows = loglikes(x, w, b, log_prior=prior)
+    r = token_logprobs(rows + prior, tokens)
+    # values of up to 30: the prior taken off and added, distance, log-probability and the rows' own rounding, u each: 150u; the log of the sum 130u
+    close(r.logprobs, want.double(), 400 * U)
+    assert float((token_logprobs(rows, tokens).logprobs - want).abs().max()) > 0.1
