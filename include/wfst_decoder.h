@@ -397,8 +397,10 @@ int32_t wfst_get_lattice_noalloc(wfst_decoder *dec, int32_t ch, const void *logl
  * themselves are read during the call.  Work is enqueued on `stream`; no call synchronises, allocates or copies to
  * the host, and every one may be recorded into a graph.  Calls from several threads and on several streams may
  * overlap, as long as none writes what another reads or writes.  Results do not depend on the launch: the same
- * call gives the same bits.  On an error nothing is enqueued, and wfst_last_error(NULL) says why (on the
- * thread that made the call).  Element types are WFST_LOGLIKE_F32 / _F16 / _BF16; sums, maxima and
+ * call gives the same bits.  On INVALID_ARG nothing is enqueued, and wfst_last_error(NULL) says why (on the
+ * thread that made the call).  Two ranges overlap if one has bytes between the other's first and last byte, used by it or
+ * not.  One launch has 2^32 work items (16 for a row of up to 256 scores, 64 up to 2,048, 256 and more behind that;
+ * 128 to 1,024 for a tile of 32 x 64 to 256 x 256 results of a product): a call of more rows than that serves is refused.  Element types are WFST_LOGLIKE_F32 / _F16 / _BF16; sums, maxima and
  * softmax statistics are held in fp32, and a 16-bit result is rounded once, at the end.  Strides count elements.
  * Errors: INVALID_ARG, HIP.
  */
@@ -407,7 +409,7 @@ enum { WFST_ACT_NONE = 0, WFST_ACT_RELU = 1, WFST_ACT_SILU = 2, WFST_ACT_GELU = 
 /*
  * y[m][n] = residual[m][n] + scale * act(sum_k x[m][k] * w[n][k] + bias[n])
  * with act one of WFST_ACT_*: none; relu max(z, 0); silu z / (1 + e^-z); gelu z/2 (1 + erf(z / sqrt 2)).
- *   rows >= 0 (0: nothing is done), k >= 1, n >= 1.  Row m of x starts at element m * x_stride (x_stride >= 0: a
+ *   rows >= 0 (0: nothing is done), 1 <= k <= 2^28, n >= 1.  Row m of x starts at element m * x_stride (x_stride >= 0: a
  *   row may be shared or overlap the next), likewise w; y_stride and residual_stride >= n.
  *   bias and residual may be NULL.  dtype: of x and w; bias_dtype: of bias; out_dtype: of y and residual.
  *   y must not overlap what is read, except that it may be the residual itself (same address and stride).
@@ -435,7 +437,7 @@ int32_t wfst_linear(const wfst_linear_args *args, void *stream);
  *   [T][B][k] tensor is taken as it is; likewise its v results (out_stride >= v; the rows must not overlap).
  *   lengths (int32 [seqs], or NULL = all frames): frames t >= lengths[s] are neither read nor written.
  *   log_prior (float [v], or NULL): log probabilities of the classes, taken off so that a hybrid decoder gets
- *   likelihoods up to a constant.  1 <= v <= 2048 (the decoder's own limit), k >= 1.
+ *   likelihoods up to a constant.  1 <= v <= 2048 (the decoder's own limit), 1 <= k <= 2^28, seqs * frames < 2^31.
  *   A frame with a NaN or +inf in z, or -inf in all of it, gives NaN for the whole row; a -inf in z gives -inf.
  */
 typedef struct {

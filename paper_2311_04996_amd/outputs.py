@@ -149,7 +149,11 @@ def _new(make, shape, dtype, dev, stream):
         return make(shape, dtype=dtype, device=dev)
 
 
-def _run(entry, args, dev, stream):
+def _run(entry, packer, fields, dev, stream):
+    try:
+        args = packer.pack(*fields)
+    except struct.error as e:
+        raise ValueError(f"a size, a stride or a number is out of range: {e}") from None
     if stream is not None:
         if stream.device.index != dev:
             raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{dev}")
@@ -202,8 +206,8 @@ def linear(x, weight, bias=None, activation=None, residual=None, scale=1.0, out=
             raise ValueError(f"residual is {residual.dtype} {tuple(residual.shape)}, the result {out.dtype} {shape}")
         _there(residual, dev, "residual")
         r, rs = residual.data_ptr(), _matrix(residual, "residual")[1]
-    _run(lib.wfst_linear, _linear.pack(x.data_ptr(), weight.data_ptr(), b, r, out.data_ptr(), rows, xs, ws, rs, ys, k, n, code, b_code,
-                                       _code(out, "out"), act, scale), dev, stream)
+    _run(lib.wfst_linear, _linear, (x.data_ptr(), weight.data_ptr(), b, r, out.data_ptr(), rows, xs, ws, rs, ys, k, n, code, b_code,
+                                    _code(out, "out"), act, scale), dev, stream)
     return out
 
 
@@ -235,8 +239,8 @@ def loglikes(hidden, weight, bias=None, log_prior=None, lengths=None, out=None, 
         raise ValueError(f"out is {out.dtype} {tuple(out.shape)}, the result {out_dtype or out.dtype} {shape}")
     _there(out, dev, "out")
     _, _, oss, os_ = _grid(out, "out")
-    _run(lib.wfst_loglikes, _loglikes.pack(hidden.data_ptr(), weight.data_ptr(), b, prior, le, out.data_ptr(), xss, xs, ws, oss, os_,
-                                           seqs, frames, k, v, code, b_code, _code(out, "out")), dev, stream)
+    _run(lib.wfst_loglikes, _loglikes, (hidden.data_ptr(), weight.data_ptr(), b, prior, le, out.data_ptr(), xss, xs, ws, oss, os_,
+                                        seqs, frames, k, v, code, b_code, _code(out, "out")), dev, stream)
     return out
 
 
@@ -277,6 +281,8 @@ def _token_logprobs(scores, tokens, top, lengths, stream):
     code = _code(scores, "scores")
     seqs, frames, ss, st = _grid(scores, "scores")
     lead, v = scores.shape[:-1], scores.shape[-1]
+    if not 0 <= top <= min(v, 64):                       # (before its results are allocated)
+        raise WfstError(-1, "wfst_token_logprobs: top must be 0 to 64, and at most v")
     le = _dense(lengths, (seqs,), torch.int32, "lengths", dev)
     new = torch.empty if lengths is None else torch.zeros
     f32, i32, on = torch.float32, torch.int32, scores.device
@@ -302,9 +308,8 @@ def _token_logprobs(scores, tokens, top, lengths, stream):
     if need > 0:
         ws = _new(torch.empty, need, torch.uint8, on, stream)
         ws_at = ws.data_ptr()
-    _run(lib.wfst_token_logprobs, _logprobs.pack(scores.data_ptr(), tok, le, lp_at, lse.data_ptr(), entropy.data_ptr(), maximum.data_ptr(),
-                                                 log_sum.data_ptr(), ids_at, tlp_at, ws_at, need, ss, st, seqs, frames, v, given, top, code),
-         dev, stream)
+    _run(lib.wfst_token_logprobs, _logprobs, (scores.data_ptr(), tok, le, lp_at, lse.data_ptr(), entropy.data_ptr(), maximum.data_ptr(),
+                                              log_sum.data_ptr(), ids_at, tlp_at, ws_at, need, ss, st, seqs, frames, v, given, top, code), dev, stream)
     return TokenLogprobs(lp, lse, entropy, maximum, log_sum, ids, tlp)
 
 
@@ -343,6 +348,6 @@ def token_logprobs_backward(scores, result, tokens=None, grad_logprobs=None, gra
         raise ValueError(f"out must be a {scores.dtype} tensor {tuple(scores.shape)}")
     _there(out, dev, "out")
     _, _, oss, ost = _grid(out, "out")
-    _run(lib.wfst_token_logprobs_backward, _backward.pack(scores.data_ptr(), tok, le, m, ls, h, ids, gl, gs, gh, gt, out.data_ptr(), ss, st, oss, ost,
-                                                          seqs, frames, v, given, top, code), dev, stream)
+    _run(lib.wfst_token_logprobs_backward, _backward, (scores.data_ptr(), tok, le, m, ls, h, ids, gl, gs, gh, gt, out.data_ptr(), ss, st, oss, ost,
+                                                       seqs, frames, v, given, top, code), dev, stream)
     return out

@@ -1,6 +1,6 @@
 """The host side of the operators beside the decoder, without a GPU: first calls from several threads, the arguments as
 bytes, the messages of failing calls, hidden states on
-another GPU."""
+another GPU, numbers that no argument holds."""
 import ctypes as C
 import os
 import sys
@@ -90,3 +90,25 @@ def test_hidden_states_on_another_gpu_than_the_current_one_are_refused(monkeypat
                  lambda: decoder.advance_hidden_partial([0, 1], Elsewhere(), [5, 5], torch.zeros(29, 8), None)):
         with pytest.raises(ValueError, match="cuda:1"):
             call()
+
+
+@pytest.mark.parametrize("where,value", [(10, 1 << 31), (10, -(1 << 31) - 1), (5, 1 << 63), (16, "1")])
+def test_numbers_that_an_argument_does_not_hold_raise_value_error(where, value):
+    fields = [0] * 17
+    fields[where] = value
+    with pytest.raises(ValueError, match="out of range"):
+        outputs._run(None, outputs._linear, fields, 0, None)
+
+
+def test_too_many_top_ones_are_refused_before_their_results_are_made(monkeypatch):
+    """2^40 of them for a few rows would be more memory than there is."""
+    import torch
+    outputs._start()
+
+    def make(*a, **kw):
+        raise AssertionError("allocated")
+
+    monkeypatch.setattr(outputs, "_new", make)
+    for top in (1 << 40, 65, 9, -1):
+        with pytest.raises(binding.WfstError, match="top must be"):
+            outputs._token_logprobs(torch.zeros(4, 8), None, top, None, None)
