@@ -85,9 +85,10 @@ int run_tiles(LinearArgs a, void *stream) {
 // 512, 512 x 2048: 18 / 13 / 10 / 6.  Half of a 64 x 64 tile, as long as there is a compute unit for each: 1,024 rows, 2048 x 512, inputs from
 // memory: 10.2, whole ones 12.2; behind that (512 x 2048): 13.8, 9.4.  Tiles of 16 x 16 with k shared out over the waves: 33 to 128 rows,
 // 2048 x 512: 7.4, 64 x 64: 9.1; 512 rows (1,024 tiles): 19, 64 x 64: 9.3.  By way of registers 256 x 256 gains nothing (511 x 2047: 482 / 476 / 531).
-// In fp32 the matrix instructions take longest, and 128 x 128 is taken where it leaves at most an eighth of the last round idle: 64 x 64 /
-// 128 x 128 at 14,803 rows, 176 x 320 (348 tiles of 128 x 128): 22 / 31, by way of registers 177 x 333: 32 / 40; 512 x 512 (464): 87 / 79;
-// 512 x 2048 (1,856): 273 / 275.
+// In fp32 the matrix instructions take longest, and 128 x 128 gains little and only where they are most of the time: rows of whole chunks, k of
+// 512 or more, results whose rows can be stored 32 bytes at a time, and at most a tenth of the last round idle.  64 x 64 / 128 x 128 (tiles of 128 x 128,
+// rounds of 256): 512 x 1024: 448: 61 / 66, 480: 67 / 66, 512: 69 / 68, 928: 125 / 127, 1,024: 134 / 128, 1,280: 174 / 159; 1024 x 256: 1,280:
+// 329 / 308; but 512 x 1021: 1,024: 136 / 169; 256 x 1024: 74 / 76; 180 x 333: 960: 67 / 86; by way of registers 177 x 1021: 64 / 98.
 template <class E> int run_linear(LinearArgs a, bool direct, void *stream) {
   if (count_tiles(a, 16, 16) <= 256) {
     a.tiles_n = (a.n - 1) / 16 + 1;
@@ -95,8 +96,7 @@ template <class E> int run_linear(LinearArgs a, bool direct, void *stream) {
   }
   if constexpr (sizeof(typename E::T) == 4) {
     const int64_t tiles = count_tiles(a, 128, 128), rounds = (tiles + 255) / 256;
-    if (tiles >= 256 && tiles * 8 >= rounds * 256 * 7)
-      return direct ? run_tiles<E, 128, 128, 64, 64, 64, 3, true>(a, stream) : run_tiles<E, 128, 128, 64, 64, 64, 3, false>(a, stream);
+    if (direct && a.k >= 512 && a.n % 8 == 0 && tiles >= 256 && tiles * 10 >= rounds * 256 * 9) return run_tiles<E, 128, 128, 64, 64, 64, 3, true>(a, stream);
     return direct ? run_tiles<E, 64, 64, 32, 32, 64, 4, true>(a, stream) : run_tiles<E, 64, 64, 32, 32, 64, 3, false>(a, stream);
   } else {
     if (direct && count_tiles(a, 256, 256) >= 256) return run_tiles<E, 256, 256, 64, 64, 64, 3, true>(a, stream);
