@@ -146,7 +146,7 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int64_t m, int col, 
 // x, and gets 16 of the 32 x 32 sums.  w is the first operand, so that the sums of a lane are of ONE row of x (lane % 32) and
 // of 4 neighbouring columns each (of 8 i + 4 (lane / 32), i = 0..3): results leave 16 bytes at a time, and a softmax
 // over the columns stays in the lane but for one exchange with lane ^ 32.
-template <class E> struct Mma {                        // 16 elements of k per step
+template <class E> struct Mma {                        // 32 bytes of k per step
   static __device__ __forceinline__ f32x16 run(i32x4 w, i32x4 x, f32x16 c);
 };
 template <> __device__ __forceinline__ f32x16 Mma<BF16>::run(i32x4 w, i32x4 x, f32x16 c) {
@@ -555,7 +555,7 @@ __device__ __forceinline__ void store4(void *p, int64_t i, int dtype, int count,
 // classes: the row's maximum and sum are the lane's own, then its neighbour's across the half wave, then, if waves lie side
 // by side (kWavesN > 1), theirs through LDS.  The log-probabilities leave from the registers, 4 neighbours at a time: a wave's
 // stores together fill whole lines of the L2.
-// Tiles differ with the number of classes and of frames; what a frame gets does not: k goes by 16 elements at a time in every one of
+// Tiles differ with the number of classes and of frames; what a frame gets does not: k goes by 32 bytes at a time in every one of
 // them, and a row's sum is that of its 32 classes at a time, in their order.
 template <class E, int BM, int BN, int WM, int WN, int ROW, int STAGES, int GROUPS, bool DIRECT, int PER_SIMD>
 __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), PER_SIMD) void loglikes_kernel(LoglikesArgs a) {

@@ -219,8 +219,9 @@ __global__ __launch_bounds__(256) void logprobs_short_kernel(LogprobsArgs a) {
 // A lane takes 16 bytes at a time, keeps the maximum of what it has seen, and scales its sums when that grows.  The top ones need
 // no list on the way: the k-th largest of the lanes' maxima (of four lanes together up to k = 32) is a bound that at least k scores reach,
 // and what reaches it lies with the lanes whose own maximum does.  Those, little more than k of 256 unless scores are equal, are
-// read again and what reaches the bound is sorted.  Rows with too many equal scores, or a NaN, have their top ones searched
-// one after the other instead.
+// read again and what reaches the bound is sorted.  Where more reach it than the list holds (a mask that leaves few scores, or equal ones), what is
+// above it is listed and the first equal ones are taken in one more reading.  Only rows with a NaN, or with more than the list holds above
+// the bound, have their top ones searched one after the other.
 constexpr int kLongThreads = 256, kLongLoads = 4, kFound = 1024;
 
 template <class E> struct Chunk {                       // 16 bytes of scores, from any address

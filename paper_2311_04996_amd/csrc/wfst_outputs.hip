@@ -84,7 +84,8 @@ int run_tiles(LinearArgs a, void *stream) {
 // 16,384, 2048 x 512: 49 / 44 / 47 / 57 (128, 256, 512, 2,048 tiles); 2,048, 2048 x 2048: 44 / 35 / 28 / 39 (64, 128, 256, 1,024);
 // 512, 512 x 2048: 18 / 13 / 10 / 6.  Half of a 64 x 64 tile, as long as there is a compute unit for each: 1,024 rows, 2048 x 512, inputs from
 // memory: 10.2, whole ones 12.2; behind that (512 x 2048): 13.8, 9.4.  Tiles of 16 x 16 with k shared out over the waves: 33 to 128 rows,
-// 2048 x 512: 7.4, 64 x 64: 9.1; 512 rows (1,024 tiles): 19, 64 x 64: 9.3.  By way of registers 256 x 256 gains nothing (511 x 2047: 482 / 476 / 531).
+// 2048 x 512: 7.4, 64 x 64: 9.1; 512 rows (1,024 tiles): 19, 64 x 64: 9.3.  By way of registers 256 x 256 gains nothing
+// (511 x 2047: 482 / 476 / 531), 64 x 64 loses more (815 where 256 x 128 takes 436).
 // In fp32 the matrix instructions take longest, and 128 x 128 gains little and only where they are most of the time: rows of whole chunks, k of
 // 512 or more, results whose rows can be stored 32 bytes at a time, and at most a tenth of the last round idle.  64 x 64 / 128 x 128 (tiles of 128 x 128,
 // rounds of 256): 512 x 1024: 448: 61 / 66, 480: 67 / 66, 512: 69 / 68, 928: 125 / 127, 1,024: 134 / 128, 1,280: 174 / 159; 1024 x 256: 1,280:
@@ -121,6 +122,10 @@ int run_rows(const LoglikesArgs &a, bool direct, void *stream) {
 // registers allow, since w is read once per tile.  Up to 256 classes the waves of a high tile have 32 rows each; else they lie
 // side by side.  us at k 512, 16 bits, low / high tiles, 129 classes: 16 frames 7.0 / 11.7, 4,096: 7.7 / 13.1, 16,384: 11.4 / 15.9,
 // 118,000: 115 / 66; 256 classes: 8.5 / 17, 9.9 / 18, 19 / 21, 197 / 86; 500: 12 / 14, 15 / 17, 35 / 27; 1,000: 20 / 24, 24 / 29, 62 / 45.
+// Behind 512 classes they go in groups: two of 512 up to 1,024; three of 384, the most that 64 rows leave registers for (of 512 they
+// spill), up to 1,152; behind that four of 512 with 32 rows, which read w twice as often.  14,800 frames, 16 bits (fp32): 600 classes: 31 (116), in groups
+// of 384: 35 (106); 1,000: 39 (147), 43 (149); 1,100: 48 (166), with 32 rows: 78 (227); 1,153: 83 (231); 1,536: 90 (257); 2,048: 113 (320).  8,192 frames of
+// 1,100: 40, with 32 rows 43; 2,048 frames: 31 to 34 both ways.
 template <class E> int run_loglikes(const LoglikesArgs &a, bool direct, void *stream) {
   const int64_t rows = (int64_t)a.seqs * a.frames;
   if (rows <= 8192) {
@@ -141,7 +146,8 @@ template <class E> int run_loglikes(const LoglikesArgs &a, bool direct, void *st
   return run_rows<E, 32, 512, 32, 64, 64, 4, 4, 2>(a, direct, stream);
 }
 
-// Long rows are cut until there are about 1,024 workgroups, into parts of 2,048 scores at least and 64 of them at most.
+// Long rows are cut until there are about 1,024 workgroups, into 64 parts at most, and so that a part has more than about 1,000 scores (up to
+// 64 parts: 2,048 at most, of 2,049 scores 1,032 and 1,017).
 int row_splits(int64_t rows, int32_t v) {
   if (v <= kShortRow) return 1;
   const int64_t most = (v - 1) / 2048 + 1, want = (1024 - 1) / rows + 1;
