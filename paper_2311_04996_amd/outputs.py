@@ -272,6 +272,9 @@ def token_logprobs(scores, tokens=None, top=0, lengths=None, stream=None):
         return _token_logprobs(scores, tokens, top, lengths, stream)
     if stream is None:
         return TokenLogprobs(*_Recorded.apply(scores, tokens, top, lengths, None))
+    for t in (scores, tokens, lengths):                  # (autograd decides when it lets go of them)
+        if t is not None and t.is_cuda:
+            t.record_stream(stream)
     with torch.cuda.stream(stream):                      # (autograd runs the backward pass on the forward's current stream)
         return TokenLogprobs(*_Recorded.apply(scores, tokens, top, lengths, stream))
 

@@ -125,6 +125,21 @@ def test_on_another_stream():
         assert torch.equal(got, want)
 
 
+def test_what_autograd_keeps_is_known_to_the_stream_that_reads_it(monkeypatch):
+    """The backward pass reads scores, tokens and lengths on the given stream after the program may have let go of them: their memory is
+    not another's before that stream is done."""
+    told = []
+    real = torch.Tensor.record_stream
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: (told.append((t.data_ptr(), s)), real(t, s))[1])
+    x = randn(gen(209), 2, 3, 50).requires_grad_()
+    tokens, lengths = torch.zeros((2, 3, 1), dtype=torch.int32, device="cuda"), torch.tensor([3, 1], dtype=torch.int32, device="cuda")
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    token_logprobs(x, tokens, lengths=lengths, stream=stream)
+    assert [(t.data_ptr(), stream) for t in (x, tokens, lengths)] == told
+    torch.cuda.synchronize()
+
+
 def test_in_a_graph_the_gradient_is_called_itself():
     g = gen(206)
     x = randn(g, 6, 3000).requires_grad_()
